@@ -57,6 +57,7 @@
 #ifndef SAE_H
 #define SAE_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -508,6 +509,138 @@ sae_status sae_predict_sessions(int32_t n, int32_t d, const uint16_t *h, const s
 #define SAE_PRED_NOALLOC_MAX_N 4096
 sae_status sae_predict_sessions_noalloc(int32_t n, int32_t d, const uint16_t *h, const sae_predictor *w,
                                         float *logit, uint8_t *pred, sae_stream_t stream);
+
+/*
+ * Paged key-value cache: the keys and values that the pool's blocks stand for,
+ * and the attention over them.
+ *
+ * A block holds the keys and values of SAE_KV_BLOCK = 16 consecutive tokens of
+ * one sequence, for one model layer (a model has one sae_kv per layer, all with
+ * the block ids of the one pool).  Per key-value head it has a page of keys, a
+ * page of values and, for an 8-bit cache, 16 + 16 scale bytes:
+ *  type          SAE_KV_BF16, SAE_KV_F16 (16-bit values) or SAE_KV_FP8 (float8
+ *                e4m3 values with one power-of-two scale per token and head)
+ *  k, v          device; block b (instance i: i * blocks_per_instance + id),
+ *                head h has its page at b * block_stride + h * 16 * head_dim
+ *                values; 16-byte aligned
+ *  block_stride  values from a block to the next one, in k and in v (a multiple
+ *                of 16 bytes), or 0 for n_kv_heads * 16 * head_dim: a larger one
+ *                lets the layers of a block lie together
+ *  k_scale, v_scale  device uint8 (FP8 only): token t of block b, head h at
+ *                b * scale_stride + 16 h + t; a byte s stands for 2^(s - 127);
+ *                16-byte aligned; scale_stride a multiple of 16, or 0 for
+ *                16 * n_kv_heads
+ *  status        device uint32 or NULL: SAE_ST_BAD_BLOCK is ORed into it where a
+ *                table holds a block id >= blocks_per_instance, an instance out of
+ *                range, or a length outside 0 .. 16 max_blocks
+ * Place of token t, dimension d in a page, with c = 16 bytes / value size:
+ *  keys    [D / c][16][c]               at [d / c][t][d % c]
+ *  values  [D / 2c][16][2][c / 8][2][4] at [d / 2c][d % 16][t / 4 % 2]
+ *                                          [d / 16 % (c / 8)][t / 8][t % 4]
+ * (the orders in which the matrix cores take them: every 16-byte load of a wave
+ * is contiguous, and neither keys nor values are transposed when they are read).
+ */
+#define SAE_KV_BLOCK 16
+enum { SAE_KV_BF16 = 0, SAE_KV_F16 = 1, SAE_KV_FP8 = 2 };
+typedef struct {
+    int32_t type;
+    int32_t n_instances;         /* 1 .. 65535                */
+    int32_t blocks_per_instance; /* 1 .. 2^24                 */
+    int32_t n_kv_heads;          /* 1 .. 256                  */
+    int32_t head_dim;            /* 64, 128 or 256            */
+    int64_t block_stride;
+    int64_t scale_stride;
+    void *k;
+    void *v;
+    uint8_t *k_scale;
+    uint8_t *v_scale;
+    uint32_t *status;
+} sae_kv;
+
+/*
+ * The sequences of one call (all arrays device int32, 4-byte aligned):
+ *  block_ids[n_seq][max_blocks]  block of tokens 16 j .. 16 j + 15 of each sequence,
+ *                     as sae_prefix_match's matched_ids has them; an entry < 0 is
+ *                     no block: its tokens are not attended to, not written, and
+ *                     read as zeros
+ *  inst[n_seq]        instance of each sequence, or NULL (instance 0)
+ *  kv_len[n_seq]      tokens of each sequence, the call's new ones included
+ *  q_start[n_seq + 1] the call's new tokens: sequence r has rows q_start[r] ..
+ *                     q_start[r + 1] - 1 of the call's arrays, the last positions
+ *                     before kv_len[r]; not decreasing, from 0 to n_tokens; or
+ *                     NULL: one new token each (n_tokens = n_seq).  A new token
+ *                     whose position would be negative (kv_len[r] smaller than the
+ *                     number of new tokens; 0 marks a padding row) has no place:
+ *                     it is not written, reads as zeros and attends to nothing
+ */
+typedef struct {
+    int32_t n_seq;      /* 0 .. 2^20 */
+    int32_t max_blocks; /* 1 .. 2^24 */
+    const int32_t *block_ids;
+    const int32_t *inst;
+    const int32_t *kv_len;
+    const int32_t *q_start;
+} sae_seqs;
+
+/*
+ * Write new tokens' keys and values to their positions.
+ *  k, v  device, [n_tokens][n_kv_heads][head_dim], values of `dtype` (SAE_KV_BF16 or
+ *        SAE_KV_F16; the cache's own type unless that is SAE_KV_FP8); k_stride and
+ *        v_stride: values from a token to the next one, >= n_kv_heads * head_dim and
+ *        a multiple of 8; 16-byte aligned
+ * A 16-bit cache gets the values as they are.  An 8-bit cache gets, per token and
+ * head, s = the smallest power of two >= 2^-126 for which no |x| / s passes 448 (1
+ * where every x is 0), and x / s rounded to the nearest e4m3 value (ties to even); a
+ * value that is not finite is stored as NaN and does not count for s.
+ * Positions written by one call must be distinct.  n_tokens: 0 .. 2^24.
+ */
+sae_status sae_kv_write(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t dtype, const void *k,
+                        int64_t k_stride, const void *v, int64_t v_stride, sae_stream_t stream);
+
+/*
+ * Read the positions that sae_kv_write would write, as plain rows (same shapes and
+ * checks; k and v are written).  An 8-bit cache's values are scaled, then rounded to
+ * dtype (exact in bf16 but for results under 2^-126; in f16 values past its largest
+ * become that one).
+ */
+sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t dtype, void *k,
+                       int64_t k_stride, void *v, int64_t v_stride, sae_stream_t stream);
+
+/*
+ * Attention of new tokens over the cache.  The query row of position p (see sae_seqs)
+ * and query head u, whose key-value head is u / (n_heads / n_kv_heads), sees the keys
+ * of positions t <= p that have a block and, with window > 0, t > p - window:
+ *   s_t = scale (q . k_t),  out = sum_t exp(s_t) v_t / sum_t exp(s_t),
+ *   lse = ln sum_t exp(s_t)
+ * with products exact, sums in fp32 (exp under the running maximum) and one rounding
+ * to the output's type.  A row that sees no key, or whose every s_t is -inf, gets
+ * zeros and lse = -inf.  What lies in a block past the sequence's last position is
+ * never used (it may be NaN).
+ *  q, out   device, [n_tokens][n_heads][head_dim] of `dtype`: the cache's type, bf16
+ *           for an FP8 cache; strides and alignment as in sae_kv_write; out may not
+ *           overlap any input
+ *  lse      device float [n_tokens][n_heads] or NULL
+ *  scale    finite
+ *  window   >= 0; 0: none
+ *  n_heads  a multiple of n_kv_heads, at most 1024
+ *  work     device scratch of at least sae_attn_work_size bytes, 16-byte aligned; the
+ *           call leaves nothing in it for later ones, so calls in stream order may share it;
+ *           calls that overlap may not
+ * sae_attn_decode takes one new token per sequence (q_start must be NULL, n_tokens =
+ * n_seq): long sequences are split over the GPU and their parts joined.
+ * sae_attn_prefill takes any number (the new tokens' keys and values are already in the
+ * cache: causal attention over the cached prefix and themselves).
+ * Results do not depend on how the work is split but for the order of fp32 sums, and
+ * that order depends on the call's arguments and lengths alone.
+ */
+sae_status sae_attn_work_size(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t n_heads,
+                              size_t *bytes);
+sae_status sae_attn_decode(const sae_kv *kv, const sae_seqs *seqs, int32_t n_heads, int32_t dtype, const void *q,
+                           int64_t q_stride, void *out, int64_t out_stride, float *lse, float scale, int32_t window,
+                           void *work, size_t work_bytes, sae_stream_t stream);
+sae_status sae_attn_prefill(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t n_heads, int32_t dtype,
+                            const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse, float scale,
+                            int32_t window, void *work, size_t work_bytes, sae_stream_t stream);
 
 /* Device realisation of the fp32 recipe's elementary functions (the ones
  * Eq. 1 and Eq. 2 are built from), element-wise, for checking it:

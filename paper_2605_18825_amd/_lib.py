@@ -70,11 +70,43 @@ class SaePool(ctypes.Structure):
         "last_access", "meta", "off", "hash", "parent", "child_count", "ref_count", "access_count")]
 
 
+class SaeKv(ctypes.Structure):
+    _fields_ = [
+        ("type", ctypes.c_int32),
+        ("n_instances", ctypes.c_int32),
+        ("blocks_per_instance", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("block_stride", ctypes.c_int64),
+        ("scale_stride", ctypes.c_int64),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("status", ctypes.c_void_p),
+    ]
+
+
+class SaeSeqs(ctypes.Structure):
+    _fields_ = [
+        ("n_seq", ctypes.c_int32),
+        ("max_blocks", ctypes.c_int32),
+        ("block_ids", ctypes.c_void_p),
+        ("inst", ctypes.c_void_p),
+        ("kv_len", ctypes.c_void_p),
+        ("q_start", ctypes.c_void_p),
+    ]
+
+
 # exported symbol -> (restype, argtypes)
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _U32 = ctypes.c_uint32
 _I64 = ctypes.c_int64
+_F32 = ctypes.c_float
+_SZ = ctypes.c_size_t
+_KV = ctypes.POINTER(SaeKv)
+_SQ = ctypes.POINTER(SaeSeqs)
 SIGNATURES = {
     "sae_status_str": (ctypes.c_char_p, [_I32]),
     "sae_last_error": (ctypes.c_char_p, [_P]),
@@ -103,6 +135,11 @@ SIGNATURES = {
     "sae_load_state": (_I32, [_P, _I32, _P, ctypes.c_size_t, _P]),
     "sae_predict_sessions": (_I32, [_I32, _I32, _P, ctypes.POINTER(SaePredictor), _P, _P, _P, _P]),
     "sae_predict_sessions_noalloc": (_I32, [_I32, _I32, _P, ctypes.POINTER(SaePredictor), _P, _P, _P]),
+    "sae_kv_write": (_I32, [_KV, _SQ, _I32, _I32, _P, _I64, _P, _I64, _P]),
+    "sae_kv_read": (_I32, [_KV, _SQ, _I32, _I32, _P, _I64, _P, _I64, _P]),
+    "sae_attn_work_size": (_I32, [_KV, _SQ, _I32, _I32, ctypes.POINTER(_SZ)]),
+    "sae_attn_decode": (_I32, [_KV, _SQ, _I32, _I32, _P, _I64, _P, _I64, _P, _F32, _I32, _P, _SZ, _P]),
+    "sae_attn_prefill": (_I32, [_KV, _SQ, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _F32, _I32, _P, _SZ, _P]),
     "sae_select_stats": (_I32, [_P, _I32, _P, _P]),
     "sae_profile_enable": (_I32, [_P, _I32]),
     "sae_profile_read": (_I32, [_P, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_I64)]),

@@ -9,7 +9,7 @@ import ctypes
 import torch
 
 from . import _lib
-from ._lib import IVL_CAP, N_BINS, SaeConfig, SaeCounters, SaeError, SaeParams, SaePool, SaePredictor  # noqa: F401
+from ._lib import IVL_CAP, N_BINS, SaeConfig, SaeCounters, SaeError, SaeKv, SaeParams, SaePool, SaePredictor, SaeSeqs  # noqa: F401
 
 KIND_EVICT_FIRST, KIND_STRUCTURAL, KIND_LOGNORMAL, KIND_RECENCY = 0, 1, 2, 3
 META_VALID, META_LEAF, META_REF = 0x40, 0x80, 0x100
@@ -290,6 +290,133 @@ def sae_predict_sessions_noalloc(h_bf16, w, logit, pred=None, stream=None):
         setattr(p, name, _ptr(w[name]).value)
     _check(None, _lib.load().sae_predict_sessions_noalloc(n, d, _ptr(h_bf16), ctypes.byref(p), _ptr(logit),
                                                           _ptr(pred), _stream(stream)))
+
+
+# ------------------------------------------------- paged key-value cache
+KV_BLOCK = 16
+KV_BF16, KV_F16, KV_FP8 = 0, 1, 2
+_KV_DTYPE = {torch.bfloat16: KV_BF16, torch.float16: KV_F16}
+
+
+def _rows(t, heads, dim):
+    """Data pointer, token stride and dtype of a [n][heads][dim] tensor of bf16 or f16 whose tokens may lie apart
+    (a slice of fused rows); its heads and dimensions are contiguous."""
+    if not t.is_cuda:
+        raise SaeError("expected a device tensor")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise SaeError("expected a tensor [n][%d][%d], got %s" % (heads, dim, tuple(t.shape)))
+    n, _, _ = t.shape
+    s0, s1, s2 = t.stride()
+    if n and (s2 != 1 or (heads > 1 and s1 != dim)):
+        raise SaeError("a token's heads must be contiguous")
+    if t.dtype not in _KV_DTYPE:
+        raise SaeError("expected bfloat16 or float16")
+    return t.data_ptr(), s0 if n > 1 else heads * dim, _KV_DTYPE[t.dtype]
+
+
+def make_kv(type, n_instances, blocks_per_instance, n_kv_heads, head_dim, k, v, k_scale=None, v_scale=None, status=None,
+            block_stride=0, scale_stride=0):
+    """One layer's paged cache over device tensors (see sae_kv in include/sae.h); it keeps them alive.  k and v are
+    bf16, f16, or 8-bit (uint8 or float8_e4m3fn) tensors of any shape that hold the cache from their first element on:
+    contiguous, or with block_stride (values) a view whose first dimension is the block."""
+    kv = SaeKv()
+    kv.type, kv.n_instances, kv.blocks_per_instance = int(type), int(n_instances), int(blocks_per_instance)
+    kv.n_kv_heads, kv.head_dim = int(n_kv_heads), int(head_dim)
+    kv.block_stride, kv.scale_stride = int(block_stride), int(scale_stride)
+    size = 1 if type == KV_FP8 else 2
+    blocks = n_instances * blocks_per_instance
+
+    def place(name, t, size, stride, block):
+        if t is None:
+            return
+        if not t.is_cuda:
+            raise SaeError("expected a device tensor")
+        if t.element_size() != size:
+            raise SaeError("%s must have %d-byte values" % (name, size))
+        if stride == 0 and not t.is_contiguous():
+            raise SaeError("expected a contiguous tensor")
+        need = ((blocks - 1) * (stride or block) + block) * size
+        if t.untyped_storage().nbytes() - t.storage_offset() * size < need:
+            raise SaeError("%s holds fewer than %d blocks" % (name, blocks))
+        setattr(kv, name, t.data_ptr())
+    place("k", k, size, kv.block_stride, n_kv_heads * KV_BLOCK * head_dim)
+    place("v", v, size, kv.block_stride, n_kv_heads * KV_BLOCK * head_dim)
+    place("k_scale", k_scale, 1, kv.scale_stride, n_kv_heads * KV_BLOCK)
+    place("v_scale", v_scale, 1, kv.scale_stride, n_kv_heads * KV_BLOCK)
+    if status is not None:
+        kv.status = _ptr(status).value
+    kv.tensors = (k, v, k_scale, v_scale, status)
+    return kv
+
+
+def make_seqs(block_ids, kv_len, q_start=None, inst=None):
+    """A call's sequences over device int32 tensors (see sae_seqs in include/sae.h); it keeps them alive.  block_ids
+    [n][max_blocks] may be the matched_ids of sae_prefix_match."""
+    n, width = block_ids.shape
+    for name, t, count in (("block_ids", block_ids, n * width), ("kv_len", kv_len, n), ("q_start", q_start, n + 1),
+                           ("inst", inst, n)):
+        if t is not None and (t.dtype != torch.int32 or t.numel() != count):
+            raise SaeError("%s must be int32 with %d elements" % (name, count))
+    s = SaeSeqs()
+    s.n_seq, s.max_blocks = n, width
+    for name, t in (("block_ids", block_ids), ("kv_len", kv_len), ("q_start", q_start), ("inst", inst)):
+        p = _ptr(t)
+        setattr(s, name, p.value if p is not None else None)
+    s.tensors = (block_ids, kv_len, q_start, inst)
+    return s
+
+
+def _kv_move(fn, kv, seqs, k, v, stream):
+    kp, ks, kt = _rows(k, kv.n_kv_heads, kv.head_dim)
+    vp, vs, vt = _rows(v, kv.n_kv_heads, kv.head_dim)
+    if kt != vt or k.shape[0] != v.shape[0]:
+        raise SaeError("k and v must have one type and one length")
+    _check(None, fn(ctypes.byref(kv), ctypes.byref(seqs), k.shape[0], kt, kp, ks, vp, vs, _stream(stream)))
+
+
+def sae_kv_write(kv, seqs, k, v, stream=None):
+    """Write the new tokens' keys and values [n][n_kv_heads][head_dim] (bf16 or f16) to their positions."""
+    _kv_move(_lib.load().sae_kv_write, kv, seqs, k, v, stream)
+
+
+def sae_kv_read(kv, seqs, k, v, stream=None):
+    """Read the positions that sae_kv_write would write into k and v."""
+    _kv_move(_lib.load().sae_kv_read, kv, seqs, k, v, stream)
+
+
+def sae_attn_work_size(kv, seqs, n_tokens, n_heads):
+    """Bytes of device scratch that an attention call of this size needs."""
+    n = ctypes.c_size_t()
+    _check(None, _lib.load().sae_attn_work_size(ctypes.byref(kv), ctypes.byref(seqs), int(n_tokens), int(n_heads),
+                                                ctypes.byref(n)))
+    return n.value
+
+
+def _attn_rows(kv, seqs, q, out, lse, work):
+    n, heads = q.shape[0], q.shape[1]
+    qp, qs, qt = _rows(q, heads, kv.head_dim)
+    op, os_, ot = _rows(out, heads, kv.head_dim)
+    if ot != qt or out.shape[0] != n:
+        raise SaeError("out must have q's type and shape")
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != n * heads):
+        raise SaeError("lse must be float32 [n][heads]")
+    return n, heads, qt, qp, qs, op, os_, _ptr(lse), _ptr(work), work.numel() * work.element_size()
+
+
+def sae_attn_decode(kv, seqs, q, out, scale, work, window=0, lse=None, stream=None):
+    """Attention of one new token per sequence: q, out [n_seq][heads][head_dim]."""
+    n, heads, ty, qp, qs, op, os_, lp, wp, wn = _attn_rows(kv, seqs, q, out, lse, work)
+    if n != seqs.n_seq:
+        raise SaeError("q must have a row per sequence")
+    _check(None, _lib.load().sae_attn_decode(ctypes.byref(kv), ctypes.byref(seqs), heads, ty, qp, qs, op, os_, lp, scale,
+                                             int(window), wp, wn, _stream(stream)))
+
+
+def sae_attn_prefill(kv, seqs, q, out, scale, work, window=0, lse=None, stream=None):
+    """Causal attention of the new tokens over their sequences' caches: q, out [n_tokens][heads][head_dim]."""
+    n, heads, ty, qp, qs, op, os_, lp, wp, wn = _attn_rows(kv, seqs, q, out, lse, work)
+    _check(None, _lib.load().sae_attn_prefill(ctypes.byref(kv), ctypes.byref(seqs), n, heads, ty, qp, qs, op, os_, lp,
+                                              scale, int(window), wp, wn, _stream(stream)))
 
 
 def status_names(bits):

@@ -1,0 +1,110 @@
+// The paged key-value cache as the kernels see it: layout, tables and the
+// lookups shared by k_kv.hip and k_attn.hip.
+#pragma once
+
+#include "sae_internal.h"
+
+// A sae_kv and a sae_seqs, checked, strides resolved to bytes.
+struct KvDev {
+    char *k, *v;
+    uint8_t *ks, *vs;
+    int64_t block_bytes;   // from a block's pages to the next block's, in k and in v
+    int64_t scale_stride;
+    const int32_t *ids, *inst, *len, *qs;
+    uint32_t *status;
+    int32_t n_inst, bpi, kvh, n_seq, max_blocks, n_tokens;
+};
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+namespace kv {
+
+__device__ __forceinline__ void report(const KvDev &c)
+{
+    if (c.status) atomicOr(c.status, (uint32_t)SAE_ST_BAD_BLOCK);
+}
+
+// Length of sequence r; one that its table cannot hold is reported and cut.
+__device__ __forceinline__ int seq_len(const KvDev &c, int r)
+{
+    const int n = c.len[r];
+    const long long most = (long long)c.max_blocks * SAE_KV_BLOCK;
+    if (n < 0 || n > most) {
+        report(c);
+        return n < 0 ? 0 : (int)most;
+    }
+    return n;
+}
+
+// First pool block of sequence r's instance, or -1.
+__device__ __forceinline__ int64_t seq_base(const KvDev &c, int r)
+{
+    const int i = c.inst ? c.inst[r] : 0;
+    if (i < 0 || i >= c.n_inst) {
+        report(c);
+        return -1;
+    }
+    return (int64_t)i * c.bpi;
+}
+
+// Pool block for table entry `id` of a sequence with that base; -1 for none.
+__device__ __forceinline__ int64_t pool_block(const KvDev &c, int64_t base, int id)
+{
+    if (id >= c.bpi) report(c);
+    return base < 0 || id < 0 || id >= c.bpi ? -1 : base + id;
+}
+
+// Rows of sequence r in the call's arrays: [first, first + count), inside
+// 0 .. n_tokens whatever q_start holds.
+__device__ __forceinline__ void seq_rows(const KvDev &c, int r, int &first, int &count)
+{
+    if (!c.qs) {
+        first = r;
+        count = 1;
+        return;
+    }
+    const int a = min(max(c.qs[r], 0), c.n_tokens), b = min(max(c.qs[r + 1], a), c.n_tokens);
+    first = a;
+    count = b - a;
+}
+
+// The sequence r with f(r) <= tile < f(r + 1), f(r) = (q_start[r] >> shift) +
+// per_seq * r, which does not decrease: 64 probes a step, one per lane (a batch
+// of up to 4,096 sequences takes two round trips).  All lanes take part.
+__device__ __forceinline__ int find_seq(const KvDev &c, int64_t tile, int shift, int per_seq)
+{
+    int lo = 0, n = c.n_seq;  // the answer lies in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + SAE_WAVE - 1) / SAE_WAVE;
+        const int r = lo + (int)__lane_id() * step;
+        const bool below = r < lo + n && (int64_t)(c.qs[r] >> shift) + (int64_t)per_seq * r <= tile;
+        const uint64_t m = __ballot(below);
+        // probes below `tile` are a prefix (lane 0's always counts)
+        const int last = m ? 63 - __clzll((long long)m) : 0;
+        const int end = lo + n;
+        lo += last * step;
+        n = min(step, end - lo);
+    }
+    return lo;
+}
+
+}  // namespace kv
+
+hipError_t launch_kv_write(const KvDev &c, int type, int dim, int dtype, const void *k, int64_t k_stride,
+                           const void *v, int64_t v_stride, hipStream_t s);
+hipError_t launch_kv_read(const KvDev &c, int type, int dim, int dtype, void *k, int64_t k_stride, void *v,
+                          int64_t v_stride, hipStream_t s);
+
+// One attention call, checked.  Strides in values.
+struct AttnArgs {
+    const void *q;
+    void *out;
+    float *lse;
+    int64_t q_stride, out_stride;
+    float scale;
+    int32_t window, heads;
+    void *work;
+};
+hipError_t launch_attn(const KvDev &c, const AttnArgs &a, int type, int dim, bool decode, hipStream_t s);
+size_t attn_work_bytes(int n_tokens, int heads, int kvh, int dim);

@@ -8,6 +8,7 @@
 #include <utility>
 #include <vector>
 
+#include "kv_cache.h"
 #include "sae_internal.h"
 
 struct sae_ctx {
@@ -526,6 +527,168 @@ sae_status sae_predict_sessions_noalloc(int32_t n, int32_t d, const uint16_t *h,
     e = launch_predict(n, d, h, w->w1, w->b1, w->w2, w->b2, w->w3, w->b3, work, logit, pred, S(stream));
     if (e != hipSuccess) return hip_fail(nullptr, e, "sae_predict_sessions_noalloc");
     return SAE_OK;
+}
+
+// ------------------------------------------------- paged key-value cache
+// Checks of a cache and of a call's sequences; fills d.  Nothing is read from
+// the device.
+static sae_status kv_args(const sae_kv *kv, const sae_seqs *sq, int32_t n_tokens, KvDev &d)
+{
+    auto bad = [](const char *msg) { return fail(nullptr, SAE_ERR_ARG, msg); };
+    if (!kv || !sq) return bad("kv and seqs must be non-NULL");
+    if (kv->type < SAE_KV_BF16 || kv->type > SAE_KV_FP8) return bad("unknown cache type");
+    if (kv->n_instances < 1 || kv->n_instances > 65535) return bad("n_instances must be in 1..65535");
+    if (kv->blocks_per_instance < 1 || kv->blocks_per_instance > (1 << 24))
+        return bad("blocks_per_instance must be in 1..2^24");
+    if (kv->n_kv_heads < 1 || kv->n_kv_heads > 256) return bad("n_kv_heads must be in 1..256");
+    if (kv->head_dim != 64 && kv->head_dim != 128 && kv->head_dim != 256) return bad("head_dim must be 64, 128 or 256");
+    const bool fp8 = kv->type == SAE_KV_FP8;
+    const int64_t size = fp8 ? 1 : 2;
+    const int64_t block = (int64_t)kv->n_kv_heads * SAE_KV_BLOCK * kv->head_dim;
+    const int64_t stride = kv->block_stride ? kv->block_stride : block;
+    if (stride < block || stride > (1ll << 38) || stride * size % 16 != 0)
+        return bad("block_stride must be 0 or a multiple of 16 bytes that holds n_kv_heads * 16 * head_dim values");
+    if (!kv->k || !kv->v || !aligned(kv->k, 16) || !aligned(kv->v, 16))
+        return bad("the cache's k and v must be non-NULL and 16-byte aligned");
+    int64_t sstride = 0;
+    if (fp8) {
+        sstride = kv->scale_stride ? kv->scale_stride : 16ll * kv->n_kv_heads;
+        if (sstride < 16ll * kv->n_kv_heads || sstride > (1ll << 38) || sstride % 16 != 0)
+            return bad("scale_stride must be 0 or a multiple of 16 that holds 16 * n_kv_heads bytes");
+        if (!kv->k_scale || !kv->v_scale || !aligned(kv->k_scale, 16) || !aligned(kv->v_scale, 16))
+            return bad("an FP8 cache needs k_scale and v_scale, 16-byte aligned");
+    }
+    if (kv->status && !aligned(kv->status, 4)) return bad("status must be 4-byte aligned");
+    if (sq->n_seq < 0 || sq->n_seq > (1 << 20)) return bad("n_seq must be in 0..2^20");
+    if (sq->max_blocks < 1 || sq->max_blocks > (1 << 24)) return bad("max_blocks must be in 1..2^24");
+    if (n_tokens < 0 || n_tokens > (1 << 24)) return bad("n_tokens must be in 0..2^24");
+    if (!sq->q_start && n_tokens != sq->n_seq) return bad("without q_start, n_tokens must be n_seq");
+    if (sq->n_seq == 0 && n_tokens != 0) return bad("tokens without a sequence");
+    if (sq->n_seq > 0 && (!sq->block_ids || !sq->kv_len)) return bad("block_ids and kv_len must be non-NULL");
+    if (!aligned(sq->block_ids, 4) || !aligned(sq->kv_len, 4) || !aligned(sq->inst, 4) || !aligned(sq->q_start, 4))
+        return bad("block_ids, inst, kv_len and q_start must be 4-byte aligned");
+    d.k = static_cast<char *>(kv->k);
+    d.v = static_cast<char *>(kv->v);
+    d.ks = kv->k_scale;
+    d.vs = kv->v_scale;
+    d.block_bytes = stride * size;
+    d.scale_stride = sstride;
+    d.ids = sq->block_ids;
+    d.inst = sq->inst;
+    d.len = sq->kv_len;
+    d.qs = sq->q_start;
+    d.status = kv->status;
+    d.n_inst = kv->n_instances;
+    d.bpi = kv->blocks_per_instance;
+    d.kvh = kv->n_kv_heads;
+    d.n_seq = sq->n_seq;
+    d.max_blocks = sq->max_blocks;
+    d.n_tokens = n_tokens;
+    return SAE_OK;
+}
+
+// An array [n][heads][dim] of 16-bit values with a stride between tokens.
+static const char *rows_args(const void *p, int64_t stride, int64_t row)
+{
+    if (!p || !aligned(p, 16)) return "row arrays must be non-NULL and 16-byte aligned";
+    if (stride < row || stride > (1ll << 38) || stride % 8 != 0)
+        return "row strides must be multiples of 8 that hold a row";
+    return nullptr;
+}
+
+static sae_status kv_move_args(const sae_kv *kv, const sae_seqs *sq, int32_t n, int32_t dtype, const void *k,
+                               int64_t k_stride, const void *v, int64_t v_stride, KvDev &d)
+{
+    sae_status st = kv_args(kv, sq, n, d);
+    if (st != SAE_OK) return st;
+    if ((dtype != SAE_KV_BF16 && dtype != SAE_KV_F16) || (kv->type != SAE_KV_FP8 && dtype != kv->type))
+        return fail(nullptr, SAE_ERR_ARG, "dtype must be the cache's type, or bf16 or f16 for an FP8 cache");
+    if (n == 0) return SAE_OK;
+    const int64_t row = (int64_t)kv->n_kv_heads * kv->head_dim;
+    const char *msg = rows_args(k, k_stride, row);
+    if (!msg) msg = rows_args(v, v_stride, row);
+    return msg ? fail(nullptr, SAE_ERR_ARG, msg) : SAE_OK;
+}
+
+sae_status sae_kv_write(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t dtype, const void *k,
+                        int64_t k_stride, const void *v, int64_t v_stride, sae_stream_t stream)
+{
+    KvDev d;
+    sae_status st = kv_move_args(kv, seqs, n_tokens, dtype, k, k_stride, v, v_stride, d);
+    if (st != SAE_OK || n_tokens == 0) return st;
+    hipError_t e = launch_kv_write(d, kv->type, kv->head_dim, dtype, k, k_stride, v, v_stride, S(stream));
+    return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, "sae_kv_write");
+}
+
+sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t dtype, void *k,
+                       int64_t k_stride, void *v, int64_t v_stride, sae_stream_t stream)
+{
+    KvDev d;
+    sae_status st = kv_move_args(kv, seqs, n_tokens, dtype, k, k_stride, v, v_stride, d);
+    if (st != SAE_OK || n_tokens == 0) return st;
+    hipError_t e = launch_kv_read(d, kv->type, kv->head_dim, dtype, k, k_stride, v, v_stride, S(stream));
+    return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, "sae_kv_read");
+}
+
+static sae_status attn_heads(const sae_kv *kv, int32_t n_heads)
+{
+    if (n_heads < 1 || n_heads > 1024 || n_heads % kv->n_kv_heads != 0)
+        return fail(nullptr, SAE_ERR_ARG, "n_heads must be a multiple of n_kv_heads in 1..1024");
+    return SAE_OK;
+}
+
+sae_status sae_attn_work_size(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t n_heads,
+                              size_t *bytes)
+{
+    KvDev d;
+    sae_status st = kv_args(kv, seqs, n_tokens, d);
+    if (st == SAE_OK) st = attn_heads(kv, n_heads);
+    if (st != SAE_OK) return st;
+    if (!bytes) return fail(nullptr, SAE_ERR_ARG, "bytes must be non-NULL");
+    *bytes = attn_work_bytes(n_tokens, n_heads, kv->n_kv_heads, kv->head_dim);
+    return SAE_OK;
+}
+
+static sae_status attn(const char *name, bool decode, const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
+                       int32_t n_heads, int32_t dtype, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                       float *lse, float scale, int32_t window, void *work, size_t work_bytes, hipStream_t s)
+{
+    KvDev d;
+    sae_status st = kv_args(kv, seqs, n_tokens, d);
+    if (st == SAE_OK) st = attn_heads(kv, n_heads);
+    if (st != SAE_OK) return st;
+    if (dtype != (kv->type == SAE_KV_FP8 ? SAE_KV_BF16 : kv->type))
+        return fail(nullptr, SAE_ERR_ARG, "dtype must be the cache's type, bf16 for an FP8 cache");
+    if (!(scale - scale == 0.0f)) return fail(nullptr, SAE_ERR_ARG, "scale must be finite");
+    if (window < 0) return fail(nullptr, SAE_ERR_ARG, "window must be >= 0");
+    if (n_tokens == 0) return SAE_OK;
+    const int64_t row = (int64_t)n_heads * kv->head_dim;
+    const char *msg = rows_args(q, q_stride, row);
+    if (!msg) msg = rows_args(out, out_stride, row);
+    if (msg) return fail(nullptr, SAE_ERR_ARG, msg);
+    if (!aligned(lse, 4)) return fail(nullptr, SAE_ERR_ARG, "lse must be 4-byte aligned");
+    if (!work || !aligned(work, 16) || work_bytes < attn_work_bytes(n_tokens, n_heads, kv->n_kv_heads, kv->head_dim))
+        return fail(nullptr, SAE_ERR_ARG, "work must be 16-byte aligned and hold sae_attn_work_size bytes");
+    const AttnArgs a = {q, out, lse, q_stride, out_stride, scale, window, n_heads, work};
+    hipError_t e = launch_attn(d, a, kv->type, kv->head_dim, decode, s);
+    return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, name);
+}
+
+sae_status sae_attn_decode(const sae_kv *kv, const sae_seqs *seqs, int32_t n_heads, int32_t dtype, const void *q,
+                           int64_t q_stride, void *out, int64_t out_stride, float *lse, float scale, int32_t window,
+                           void *work, size_t work_bytes, sae_stream_t stream)
+{
+    if (seqs && seqs->q_start) return fail(nullptr, SAE_ERR_ARG, "sae_attn_decode takes no q_start");
+    return attn("sae_attn_decode", true, kv, seqs, seqs ? seqs->n_seq : 0, n_heads, dtype, q, q_stride, out, out_stride,
+                lse, scale, window, work, work_bytes, S(stream));
+}
+
+sae_status sae_attn_prefill(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t n_heads, int32_t dtype,
+                            const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse, float scale,
+                            int32_t window, void *work, size_t work_bytes, sae_stream_t stream)
+{
+    return attn("sae_attn_prefill", false, kv, seqs, n_tokens, n_heads, dtype, q, q_stride, out, out_stride, lse, scale,
+                window, work, work_bytes, S(stream));
 }
 
 sae_status sae_block_type(const uint8_t *counts, int64_t n, uint8_t *tau, sae_stream_t stream)
