@@ -100,10 +100,11 @@ void launch_dim(const KvDev &c, const AttnArgs &a, int dim, hipStream_t s)
 
 }  // namespace
 
-size_t attn_work_bytes(int, int, int, int) { return 256; }
+size_t attn_work_bytes(int, int heads, int kvh, int dim) { return decode_work_bytes(heads, kvh, dim); }
 
-hipError_t launch_attn(const KvDev &c, const AttnArgs &a, int type, int dim, bool, hipStream_t s)
+hipError_t launch_attn(const KvDev &c, const AttnArgs &a, int type, int dim, bool decode, hipStream_t s)
 {
+    if (decode) return launch_decode(c, a, type, dim, s);
     if (type == SAE_KV_BF16) launch_dim<SAE_KV_BF16>(c, a, dim, s);
     else if (type == SAE_KV_F16) launch_dim<SAE_KV_F16>(c, a, dim, s);
     else launch_dim<SAE_KV_FP8>(c, a, dim, s);

@@ -1,0 +1,555 @@
+// Attention of one new token per sequence over the paged key-value cache.
+//
+// Per sequence and key-value head, with the G query heads that share it as the
+// columns of a 16-wide matrix (G of them used; more than 16 take several tiles):
+//   S^T = K Q^T (32 keys x 16 heads a step), P = exp(S - m), O^T += V^T P^T
+// on v_mfma_f32_16x16x32, m and the sum of P running (one pass over the keys).
+// The time is that of reading the cache once: the matrix units are used because
+// they take every cached byte from the register it was loaded into, for 16 heads
+// at the price of one.
+//
+// Everything stays in registers: lane (n = lane % 16, g = lane / 16) holds the
+// scores of head n for 8 of the 32 keys, and the same 8 keys are what lane
+// group g supplies of V^T and P^T to the second product, because the 32 rows of
+// K are taken in the order that makes it so (below) and because the sum over
+// keys may be taken in any order that both operands share.  So neither P nor
+// the output passes through LDS or other lanes; the running maximum needs two
+// swaps across lane groups a step.
+//   first product, tile u = 0, 1: row 4 g' + i is token 8 u + 4 (g' % 2) + i of
+//     page g' / 2 of the step's two pages
+//   second product: k = 8 g + j is, for j < 4, token 4 (g % 2) + j of page g / 2,
+//     for j >= 4 token 8 + 4 (g % 2) + j - 4: the 8 tokens of a value page's
+//     16-byte piece.
+//
+// Work is divided evenly whatever the lengths: all sequences' steps lie one
+// after the other, and workgroup x takes steps x per .. (x + 1) per - 1 of its
+// head, found from the lengths alone (a scan in every workgroup: the host knows
+// no lengths, and a captured call keeps fitting as they grow).  A sequence that
+// lies in one workgroup is finished there; the parts of others go to the
+// workspace and k_decode_join adds them.  A workgroup has at most two such
+// parts: its first sequence's end and its last one's beginning.
+#include "kv_cache.h"
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int NW = 4, THREADS = NW * SAE_WAVE;
+constexpr int STEP = 32;       // keys a wave takes at a time: two pages
+constexpr int COLS = 16;       // query heads of a tile
+constexpr int MIN_STEPS = NW;  // steps of a workgroup at least (where there are as many)
+constexpr int GROUPS = 512;    // workgroups of a call, about: two per compute unit
+constexpr float NEG_INF = -__builtin_inff();
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
+
+template <int TYPE>
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
+{
+    if constexpr (TYPE == SAE_KV_F16) {
+        f16x8 x, y;
+        __builtin_memcpy(&x, &a, 16);
+        __builtin_memcpy(&y, &b, 16);
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
+    } else {
+        bf16x8 x, y;
+        __builtin_memcpy(&x, &a, 16);
+        __builtin_memcpy(&y, &b, 16);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+    }
+}
+
+// 8 e4m3 values as bf16 (exact).
+__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi)
+{
+    const bf16x2 t[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true)};
+    u32x4 r;
+    __builtin_memcpy(&r, t, 16);
+    return r;
+}
+
+// Two values rounded to the 16-bit type, and what the rounding left, rounded too.
+template <int TYPE>
+__device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo)
+{
+    if constexpr (TYPE == SAE_KV_F16) {
+        _Float16 h[2] = {(_Float16)a, (_Float16)b}, l[2] = {(_Float16)(a - (float)h[0]), (_Float16)(b - (float)h[1])};
+        __builtin_memcpy(&hi, h, 4);
+        __builtin_memcpy(&lo, l, 4);
+    } else {
+        __bf16 h[2] = {(__bf16)a, (__bf16)b}, l[2] = {(__bf16)(a - (float)h[0]), (__bf16)(b - (float)h[1])};
+        __builtin_memcpy(&hi, h, 4);
+        __builtin_memcpy(&lo, l, 4);
+    }
+}
+
+// Maximum over the four lane groups (lanes that agree mod 16).
+__device__ __forceinline__ float max_groups(float x)
+{
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+__device__ __forceinline__ float sum_groups(float x)
+{
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// First key and number of steps of a sequence of n tokens (one step, which
+// sees nothing, where there is no key: its workgroup writes the zeros).
+__device__ __forceinline__ int first_key(int n, int window) { return window > 0 && n > window ? n - window : 0; }
+__device__ __forceinline__ int steps_of(int n, int window)
+{
+    return n <= 0 ? 1 : (n + STEP - 1) / STEP - first_key(n, window) / STEP;
+}
+
+// Steps per workgroup, for `total` steps over `groups` workgroups.
+__device__ __forceinline__ long long steps_per(long long total, int groups)
+{
+    const long long p = (total + groups - 1) / groups;
+    return p < MIN_STEPS ? MIN_STEPS : p;
+}
+
+// Where workgroup x of a head starts: its first sequence and the step in it.
+struct Start {
+    long long per, begin, end;  // steps begin .. end - 1 of all
+    int seq;
+    long long seq_at;           // number of that sequence's first step
+};
+
+// Exclusive scan over the workgroup's threads; total in every thread.
+__device__ __forceinline__ long long scan(long long v, long long &total, long long *lds)
+{
+    const int lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
+    long long s = v;
+#pragma unroll
+    for (int o = 1; o < SAE_WAVE; o <<= 1) {
+        const long long u = __shfl_up(s, o);
+        if (lane >= o) s += u;
+    }
+    if (lane == SAE_WAVE - 1) lds[wave] = s;
+    __syncthreads();
+    long long before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        if (w < wave) before += lds[w];
+        total += lds[w];
+    }
+    __syncthreads();
+    return before + s - v;
+}
+
+__device__ __forceinline__ Start find_start(const KvDev &c, int window, int x, int groups)
+{
+    __shared__ long long tmp[NW];
+    __shared__ long long found_at;
+    __shared__ int found_seq;
+    const int n = c.n_seq, chunk = (n + THREADS - 1) / THREADS;
+    const int r0 = min((int)threadIdx.x * chunk, n), r1 = min(r0 + chunk, n);
+    long long sum = 0;
+    for (int r = r0; r < r1; ++r) sum += steps_of(kv::seq_len(c, r), window);
+    Start s;
+    long long total;
+    long long at = scan(sum, total, tmp);
+    s.per = steps_per(total, groups);
+    s.begin = x * s.per;
+    s.end = min(s.begin + s.per, total);
+    if (s.begin < total && at <= s.begin && s.begin < at + sum) {  // one thread
+        int r = r0;
+        for (;; ++r) {
+            const int k = steps_of(kv::seq_len(c, r), window);
+            if (s.begin < at + k) break;
+            at += k;
+        }
+        found_seq = r;
+        found_at = at;
+    }
+    __syncthreads();
+    s.seq = s.begin < total ? found_seq : n;
+    s.seq_at = s.begin < total ? found_at : total;
+    return s;
+}
+
+// Workspace: per workgroup x a description of the sequence that begins in it
+// and ends in a later one, then per (x, head tile, slot) 16 maxima, 16 sums and
+// 16 rows of unnormalised outputs.
+struct Part {
+    int seq, count;  // parts of that sequence: workgroups x .. x + count - 1; seq < 0: none
+};
+__host__ __device__ constexpr size_t part_floats(int dim) { return (size_t)COLS * (dim + 2); }
+__host__ __device__ constexpr size_t meta_bytes(int groups) { return ((size_t)groups * sizeof(Part) + 15) / 16 * 16; }
+
+struct Shape {
+    int groups, tiles, per_kv;  // workgroups per head tile; head tiles in all; head tiles of a key-value head
+};
+
+// One step's keys and values of a lane, as loaded.
+template <int TYPE, int D>
+struct Frag {
+    static constexpr int NK = TYPE == SAE_KV_FP8 ? D / 64 : D / 32;  // pieces of a row tile
+    static constexpr int NV = TYPE == SAE_KV_FP8 ? D / 32 : D / 16;
+    u32x4 k[2][NK], v[NV];
+    uint32_t ks[2], vs[2];  // scale bytes of the lane's 8 keys
+};
+
+template <int TYPE, int D>
+__global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, AttnArgs a, Shape sh)
+{
+    constexpr bool FP8 = TYPE == SAE_KV_FP8;
+    constexpr int E = FP8 ? 1 : 2, PAGE = SAE_KV_BLOCK * D * E;
+    constexpr int NO = D / 16, NQ = D / 32;
+    typedef Frag<TYPE, D> F;
+    constexpr int OROW = D + 4;  // LDS row of an output, padded against conflicts
+    __shared__ float ox[NW][COLS][OROW];
+    __shared__ float mx[NW][COLS], lx[NW][COLS];
+
+    const int x = blockIdx.x, tile = blockIdx.y;
+    const int kvhead = tile / sh.per_kv, G = a.heads / c.kvh;
+    const int head0 = kvhead * G + tile % sh.per_kv * COLS;
+    const int cols = min(COLS, G - tile % sh.per_kv * COLS);
+    const int lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
+    const int n = lane & 15, g = lane >> 4;
+    const Start st = find_start(c, a.window, x, sh.groups);
+    Part *meta = reinterpret_cast<Part *>(a.work);
+    float *parts = reinterpret_cast<float *>(static_cast<char *>(a.work) + meta_bytes(sh.groups));
+    Part mine = {-1, 0};
+    const float sl = a.scale * LOG2E;
+    // the lane's place in a page (bytes)
+    const int koff = g * 256 + (lane & 7) * 16, voff = (lane & 15) * 32 + (g & 1) * 16;
+    const bool kpage = lane & 8, vpage = lane & 32;
+
+    long long at = st.begin, seq_at = st.seq_at;
+    for (int r = st.seq; at < st.end; ++r) {
+        const int len = kv::seq_len(c, r), total = steps_of(len, a.window);
+        const int lo = first_key(len, a.window);
+        const int s0 = (int)(at - seq_at), s1 = (int)min((long long)total, st.end - seq_at);
+        const int step0 = lo / STEP;  // in steps of the whole sequence
+        const int64_t base = kv::seq_base(c, r);
+        u32x4 q[NQ];
+        {
+            const char *qr = static_cast<const char *>(a.q) + ((int64_t)r * a.q_stride + (int64_t)(head0 + n) * D) * 2;
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                // 8-bit keys come 16 dimensions a piece: piece i / 2 of lane group g, its half i % 2
+                const int d = FP8 ? i / 2 * 64 + g * 16 + i % 2 * 8 : i * 32 + g * 8;
+                q[i] = u32x4{0, 0, 0, 0};
+                if (n < cols) q[i] = *reinterpret_cast<const u32x4 *>(qr + d * 2);
+            }
+        }
+        f32x4 o[NO];
+#pragma unroll
+        for (int i = 0; i < NO; ++i) o[i] = f32x4{0, 0, 0, 0};
+        float m = NEG_INF, l = 0.0f;
+
+        // table entries of the wave's next 32 steps: lane 2 j + u has page u of step j
+        int ids = -1, ids_from = -1;
+        const int count = (s1 - s0 - wave + NW - 1) / NW;  // this wave's steps: s0 + wave + NW j
+        auto fetch = [&](F &f, int j, bool &v0, bool &v1) {
+            if (j >= count) return;
+            if (ids_from < 0 || j >= ids_from + 32) {  // uniform
+                ids_from = j;
+                const int page = 2 * (step0 + s0 + wave + NW * (j + (lane >> 1))) + (lane & 1);
+                ids = -1;
+                if (j + (lane >> 1) < count && page * SAE_KV_BLOCK < len)
+                    ids = c.ids[(int64_t)r * c.max_blocks + page];
+                if (ids >= c.bpi) kv::report(c);
+                if (base < 0 || ids >= c.bpi) ids = -1;
+            }
+            const int i0 = __builtin_amdgcn_readlane(ids, 2 * (j - ids_from));
+            const int i1 = __builtin_amdgcn_readlane(ids, 2 * (j - ids_from) + 1);
+            v0 = i0 >= 0;
+            v1 = i1 >= 0;
+            // a page that is not there is read as block 0, and masked
+            const int64_t b0 = v0 ? base + i0 : 0, b1 = v1 ? base + i1 : 0;
+            const int64_t a0 = b0 * c.block_bytes + (int64_t)kvhead * PAGE, a1 = b1 * c.block_bytes + (int64_t)kvhead * PAGE;
+            const char *kp = c.k + (kpage ? a1 : a0) + koff, *vp = c.v + (vpage ? a1 : a0) + voff;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < F::NK; ++i) f.k[u][i] = *reinterpret_cast<const u32x4 *>(kp + i * 1024 + u * 128);
+#pragma unroll
+            for (int i = 0; i < F::NV; ++i) f.v[i] = *reinterpret_cast<const u32x4 *>(vp + i * 512);
+            if constexpr (FP8) {
+                const int64_t s = (vpage ? b1 : b0) * c.scale_stride + kvhead * SAE_KV_BLOCK + (g & 1) * 4;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    f.ks[u] = *reinterpret_cast<const uint32_t *>(c.ks + s + u * 8);
+                    f.vs[u] = *reinterpret_cast<const uint32_t *>(c.vs + s + u * 8);
+                }
+            }
+        };
+        auto compute = [&](F &f, int j, bool v0, bool v1) {
+            const int t0 = (step0 + s0 + wave + NW * j) * STEP;
+            f32x4 s[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                s[u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < F::NK; ++i) {
+                    if constexpr (FP8) {
+                        s[u] = mfma<SAE_KV_BF16>(widen(f.k[u][i][0], f.k[u][i][1]), q[2 * i], s[u]);
+                        s[u] = mfma<SAE_KV_BF16>(widen(f.k[u][i][2], f.k[u][i][3]), q[2 * i + 1], s[u]);
+                    } else {
+                        s[u] = mfma<TYPE>(f.k[u][i], q[i], s[u]);
+                    }
+                }
+            }
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w[e] = s[e / 4][e % 4] * sl;
+                if constexpr (FP8) w[e] *= __uint_as_float(((f.ks[e / 4] >> (8 * (e % 4))) & 0xFFu) << 23);
+            }
+            if (!v0 || !v1 || t0 < lo || t0 + STEP > len) {  // uniform: some key of the step is not seen
+                const bool there = vpage ? v1 : v0;
+                const int tl = t0 + (g >> 1) * SAE_KV_BLOCK + (g & 1) * 4;
+                uint32_t keep = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int t = tl + (e / 4) * 8 + e % 4;
+                    if (there && t >= lo && t < len) keep |= 1u << e;
+                    else w[e] = NEG_INF;
+                }
+                // a value that is not seen may be NaN: it becomes 0
+#pragma unroll
+                for (int i = 0; i < F::NV; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if constexpr (FP8) {  // bytes: 8 keys of one dimension, then of another
+#pragma unroll
+                            for (int b = 0; b < 4; ++b)
+                                if (!(keep >> (4 * (k & 1) + b) & 1)) f.v[i][k] &= ~(0xFFu << (8 * b));
+                        } else {
+#pragma unroll
+                            for (int b = 0; b < 2; ++b)
+                                if (!(keep >> (2 * k + b) & 1)) f.v[i][k] &= ~(0xFFFFu << (16 * b));
+                        }
+                    }
+                if constexpr (FP8) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!(keep >> e & 1)) f.vs[e / 4] &= ~(0xFFu << (8 * (e % 4)));  // its scale byte too
+                }
+            }
+            float top = w[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) top = fmaxf(top, w[e]);
+            top = max_groups(top);
+            if (__any(top > m)) {  // a head's maximum grew: what is summed so far shrinks
+                const float mn = fmaxf(m, top);
+                const float f0 = mn == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= f0;
+#pragma unroll
+                for (int i = 0; i < NO; ++i) o[i] *= f0;
+            }
+            const float mu = m == NEG_INF ? 0.0f : m;  // nothing seen yet
+            u32x4 hi, lo_;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w[e] = __builtin_amdgcn_exp2f(w[e] - mu);
+                l += w[e];
+                if constexpr (FP8) w[e] *= __uint_as_float(((f.vs[e / 4] >> (8 * (e % 4))) & 0xFFu) << 23);
+            }
+            // the weights as two 16-bit numbers each: the product with the values
+            // costs twice the (idle) matrix units and keeps 16 bits or more of them
+            constexpr int PT = TYPE == SAE_KV_F16 ? SAE_KV_F16 : SAE_KV_BF16;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t h_, l_;
+                split2<PT>(w[2 * e], w[2 * e + 1], h_, l_);
+                hi[e] = h_;
+                lo_[e] = l_;
+            }
+#pragma unroll
+            for (int i = 0; i < NO; ++i) {
+                const u32x4 v = FP8 ? widen(f.v[i / 2][i % 2 * 2], f.v[i / 2][i % 2 * 2 + 1]) : f.v[FP8 ? 0 : i];
+                o[i] = mfma<PT>(v, hi, o[i]);
+                o[i] = mfma<PT>(v, lo_, o[i]);
+            }
+        };
+        // the next step's loads are in flight while one is computed
+        F f0, f1;
+        bool va0 = false, va1 = false, vb0 = false, vb1 = false;
+        fetch(f0, 0, va0, va1);
+        for (int j = 0; j < count; j += 2) {
+            fetch(f1, j + 1, vb0, vb1);
+            compute(f0, j, va0, va1);
+            if (j + 1 < count) {
+                fetch(f0, j + 2, va0, va1);
+                compute(f1, j + 1, vb0, vb1);
+            }
+        }
+
+        // the waves' parts: common maximum, sums, outputs
+        l = sum_groups(l);
+        __syncthreads();  // the last sequence's sums have been read
+        if (g == 0) {
+            mx[wave][n] = m;
+            lx[wave][n] = l;
+        }
+#pragma unroll
+        for (int i = 0; i < NO; ++i) *reinterpret_cast<f32x4 *>(&ox[wave][n][i * 16 + g * 4]) = o[i];
+        __syncthreads();
+        const bool whole = s0 == 0 && s1 == total;
+        const size_t slot = ((size_t)x * sh.tiles + tile) * 2 + (s0 == 0 ? 1 : 0);
+        float *pm = parts + slot * part_floats(D), *po = pm + 2 * COLS;
+        for (int i = threadIdx.x; i < cols * (D / 4); i += THREADS) {
+            const int h = i / (D / 4), d = i % (D / 4) * 4;
+            float top = NEG_INF;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) top = fmaxf(top, mx[w][h]);
+            f32x4 sum = {0, 0, 0, 0};
+            float z = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float f = mx[w][h] == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(mx[w][h] - top);
+                z += lx[w][h] * f;
+                sum += *reinterpret_cast<const f32x4 *>(&ox[w][h][d]) * f;
+            }
+            if (whole) {
+                const float inv = z == 0.0f ? 0.0f : 1.0f / z;  // no key, or every score -inf
+                const int64_t to = (int64_t)r * a.out_stride + (int64_t)(head0 + h) * D + d;
+                u32x2 b;
+                if constexpr (TYPE == SAE_KV_F16) {
+                    _Float16 y[4] = {(_Float16)(sum[0] * inv), (_Float16)(sum[1] * inv), (_Float16)(sum[2] * inv),
+                                     (_Float16)(sum[3] * inv)};
+                    __builtin_memcpy(&b, y, 8);
+                } else {
+                    __bf16 y[4] = {(__bf16)(sum[0] * inv), (__bf16)(sum[1] * inv), (__bf16)(sum[2] * inv),
+                                   (__bf16)(sum[3] * inv)};
+                    __builtin_memcpy(&b, y, 8);
+                }
+                *reinterpret_cast<u32x2 *>(static_cast<char *>(a.out) + to * 2) = b;
+                if (a.lse && d == 0)
+                    a.lse[(int64_t)r * a.heads + head0 + h] = z == 0.0f ? NEG_INF : (top + __builtin_amdgcn_logf(z)) * LN2;
+            } else {
+                *reinterpret_cast<f32x4 *>(po + h * D + d) = sum;
+                if (d == 0) {
+                    pm[h] = top;
+                    pm[COLS + h] = z;
+                }
+            }
+        }
+        if (s0 == 0 && s1 < total) {
+            mine.seq = r;
+            mine.count = (int)((seq_at + total - 1) / st.per) - x + 1;
+        }
+        at = seq_at + s1;
+        seq_at += total;
+    }
+    if (tile == 0 && threadIdx.x == 0) meta[x] = mine;
+}
+
+// Joins the parts of the sequence that begins in workgroup x and ends in a
+// later one: one workgroup per (x, query head), its threads in JR rows of D / 4,
+// row i taking parts i, i + JR, ...
+template <int TYPE, int D>
+__global__ void __launch_bounds__(THREADS) k_decode_join(KvDev c, AttnArgs a, Shape sh)
+{
+    constexpr int LD = D / 4, JR = THREADS / LD;
+    __shared__ float mz[JR], zz[JR];
+    __shared__ f32x4 oz[JR][LD];
+    const int x = blockIdx.x, head = blockIdx.y;
+    const Part p = reinterpret_cast<const Part *>(a.work)[x];
+    if (p.seq < 0) return;
+    const float *parts = reinterpret_cast<const float *>(static_cast<const char *>(a.work) + meta_bytes(sh.groups));
+    const int G = a.heads / c.kvh, u = head % G;
+    const int tile = head / G * sh.per_kv + u / COLS, h = u % COLS;
+    const int row = threadIdx.x / LD, d = threadIdx.x % LD;
+    float m = NEG_INF, z = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    for (int i = row; i < p.count; i += JR) {
+        const float *pm = parts + (((size_t)(x + i) * sh.tiles + tile) * 2 + (i == 0 ? 1 : 0)) * part_floats(D);
+        const float mi = pm[h], zi = pm[COLS + h];
+        const f32x4 oi = *reinterpret_cast<const f32x4 *>(pm + 2 * COLS + h * D + d * 4);
+        const float top = fmaxf(m, mi), mu = top == NEG_INF ? 0.0f : top;
+        const float fo = __builtin_amdgcn_exp2f(m - mu), fi = __builtin_amdgcn_exp2f(mi - mu);
+        o = o * fo + oi * fi;
+        z = z * fo + zi * fi;
+        m = top;
+    }
+    if (d == 0) {
+        mz[row] = m;
+        zz[row] = z;
+    }
+    oz[row][d] = o;
+    __syncthreads();
+    if (row != 0) return;
+    float top = NEG_INF;
+#pragma unroll
+    for (int i = 0; i < JR; ++i) top = fmaxf(top, mz[i]);
+    const float mu = top == NEG_INF ? 0.0f : top;
+    z = 0.0f;
+    o = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < JR; ++i) {
+        const float f = __builtin_amdgcn_exp2f(mz[i] - mu);
+        z += zz[i] * f;
+        o += oz[i][d] * f;
+    }
+    const float inv = z == 0.0f ? 0.0f : 1.0f / z;
+    const int64_t to = (int64_t)p.seq * a.out_stride + (int64_t)head * D + d * 4;
+    u32x2 b;
+    if constexpr (TYPE == SAE_KV_F16) {
+        _Float16 y[4] = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
+        __builtin_memcpy(&b, y, 8);
+    } else {
+        __bf16 y[4] = {(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv), (__bf16)(o[3] * inv)};
+        __builtin_memcpy(&b, y, 8);
+    }
+    *reinterpret_cast<u32x2 *>(static_cast<char *>(a.out) + to * 2) = b;
+    if (a.lse && d == 0)
+        a.lse[(int64_t)p.seq * a.heads + head] = z == 0.0f ? NEG_INF : (top + __builtin_amdgcn_logf(z)) * LN2;
+}
+
+Shape shape_of(int heads, int kvh)
+{
+    Shape s;
+    s.per_kv = (heads / kvh + COLS - 1) / COLS;
+    s.tiles = kvh * s.per_kv;
+    s.groups = GROUPS / s.tiles > 1 ? GROUPS / s.tiles : 1;
+    return s;
+}
+
+template <int TYPE, int D>
+hipError_t launch(const KvDev &c, const AttnArgs &a, hipStream_t s)
+{
+    const Shape sh = shape_of(a.heads, c.kvh);
+    hipLaunchKernelGGL((k_decode<TYPE, D>), dim3(sh.groups, sh.tiles), dim3(THREADS), 0, s, c, a, sh);
+    hipError_t e = hipGetLastError();
+    // one workgroup per head: no sequence is split
+    if (e != hipSuccess || sh.groups == 1) return e;
+    hipLaunchKernelGGL((k_decode_join<TYPE, D>), dim3(sh.groups, a.heads), dim3(THREADS), 0, s, c, a, sh);
+    return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t launch_dim(const KvDev &c, const AttnArgs &a, int dim, hipStream_t s)
+{
+    return dim == 64 ? launch<TYPE, 64>(c, a, s) : dim == 128 ? launch<TYPE, 128>(c, a, s) : launch<TYPE, 256>(c, a, s);
+}
+
+}  // namespace
+
+size_t decode_work_bytes(int heads, int kvh, int dim)
+{
+    const Shape s = shape_of(heads, kvh);
+    return meta_bytes(s.groups) + (size_t)s.groups * s.tiles * 2 * part_floats(dim) * sizeof(float);
+}
+
+hipError_t launch_decode(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s)
+{
+    if (type == SAE_KV_BF16) return launch_dim<SAE_KV_BF16>(c, a, dim, s);
+    if (type == SAE_KV_F16) return launch_dim<SAE_KV_F16>(c, a, dim, s);
+    return launch_dim<SAE_KV_FP8>(c, a, dim, s);
+}

@@ -107,4 +107,6 @@ struct AttnArgs {
     void *work;
 };
 hipError_t launch_attn(const KvDev &c, const AttnArgs &a, int type, int dim, bool decode, hipStream_t s);
+hipError_t launch_decode(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s);
+size_t decode_work_bytes(int heads, int kvh, int dim);
 size_t attn_work_bytes(int n_tokens, int heads, int kvh, int dim);
