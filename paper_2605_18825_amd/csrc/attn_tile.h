@@ -1,0 +1,90 @@
+// What the attention kernels share: matrix products by cache type, conversions
+// and reductions over lane groups.
+#pragma once
+
+#include "kv_cache.h"
+
+namespace attn {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr float NEG_INF = -__builtin_inff();
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
+
+// The 16-bit type that products of a cache type are taken in.
+constexpr bool is_f16(int type) { return type == SAE_KV_F16; }
+
+template <bool F16>
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
+{
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c)
+{
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Two values rounded to the 16-bit type (nearest even).
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if constexpr (F16) return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+    else return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+}
+
+// The two values of a packed pair.
+template <bool F16>
+__device__ __forceinline__ float low(uint32_t x)
+{
+    if constexpr (F16) return (float)__builtin_bit_cast(f16x2, x)[0];
+    else return __uint_as_float(x << 16);
+}
+template <bool F16>
+__device__ __forceinline__ float high(uint32_t x)
+{
+    if constexpr (F16) return (float)__builtin_bit_cast(f16x2, x)[1];
+    else return __uint_as_float(x & 0xFFFF0000u);
+}
+
+// Four e4m3 values times a power of two, as bf16 (exact but for results under 2^-126).
+__device__ __forceinline__ u32x2 widen4(uint32_t x, float scale)
+{
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true))};
+}
+__device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi, float scale)
+{
+    const u32x2 a = widen4(lo, scale), b = widen4(hi, scale);
+    return u32x4{a[0], a[1], b[0], b[1]};
+}
+
+// 2^(s - 127) for byte i of a word of scale bytes.
+__device__ __forceinline__ float scale_of(uint32_t word, int i) { return __uint_as_float(((word >> (8 * i)) & 0xFFu) << 23); }
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
+
+// Maximum over lanes l and l ^ 32.
+__device__ __forceinline__ float max_halves(float x)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+// Maximum over the four lanes that agree mod 16.
+__device__ __forceinline__ float max_groups(float x)
+{
+    x = max_halves(x);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+}  // namespace attn

@@ -28,73 +28,23 @@
 // lies in one workgroup is finished there; the parts of others go to the
 // workspace and k_decode_join adds them.  A workgroup has at most two such
 // parts: its first sequence's end and its last one's beginning.
-#include "kv_cache.h"
+#include "attn_tile.h"
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+using namespace attn;
 
 constexpr int NW = 4, THREADS = NW * SAE_WAVE;
 constexpr int STEP = 32;       // keys a wave takes at a time: two pages
 constexpr int COLS = 16;       // query heads of a tile
 constexpr int MIN_STEPS = NW;  // steps of a workgroup at least (where there are as many)
 constexpr int GROUPS = 512;    // workgroups of a call, about: two per compute unit
-constexpr float NEG_INF = -__builtin_inff();
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
-
-template <int TYPE>
-__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
-{
-    if constexpr (TYPE == SAE_KV_F16) {
-        f16x8 x, y;
-        __builtin_memcpy(&x, &a, 16);
-        __builtin_memcpy(&y, &b, 16);
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
-    } else {
-        bf16x8 x, y;
-        __builtin_memcpy(&x, &a, 16);
-        __builtin_memcpy(&y, &b, 16);
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
-    }
-}
-
-// 8 e4m3 values as bf16 (exact).
-__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi)
-{
-    const bf16x2 t[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true)};
-    u32x4 r;
-    __builtin_memcpy(&r, t, 16);
-    return r;
-}
-
 // Two values rounded to the 16-bit type, and what the rounding left, rounded too.
-template <int TYPE>
+template <bool F16>
 __device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo)
 {
-    if constexpr (TYPE == SAE_KV_F16) {
-        _Float16 h[2] = {(_Float16)a, (_Float16)b}, l[2] = {(_Float16)(a - (float)h[0]), (_Float16)(b - (float)h[1])};
-        __builtin_memcpy(&hi, h, 4);
-        __builtin_memcpy(&lo, l, 4);
-    } else {
-        __bf16 h[2] = {(__bf16)a, (__bf16)b}, l[2] = {(__bf16)(a - (float)h[0]), (__bf16)(b - (float)h[1])};
-        __builtin_memcpy(&hi, h, 4);
-        __builtin_memcpy(&lo, l, 4);
-    }
-}
-
-// Maximum over the four lane groups (lanes that agree mod 16).
-__device__ __forceinline__ float max_groups(float x)
-{
-    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    hi = pack2<F16>(a, b);
+    lo = pack2<F16>(a - low<F16>(hi), b - high<F16>(hi));
 }
 
 __device__ __forceinline__ float sum_groups(float x)
@@ -204,7 +154,7 @@ struct Frag {
 template <int TYPE, int D>
 __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, AttnArgs a, Shape sh)
 {
-    constexpr bool FP8 = TYPE == SAE_KV_FP8;
+    constexpr bool FP8 = TYPE == SAE_KV_FP8, F16 = is_f16(TYPE);
     constexpr int E = FP8 ? 1 : 2, PAGE = SAE_KV_BLOCK * D * E;
     constexpr int NO = D / 16, NQ = D / 32;
     typedef Frag<TYPE, D> F;
@@ -296,10 +246,10 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
 #pragma unroll
                 for (int i = 0; i < F::NK; ++i) {
                     if constexpr (FP8) {
-                        s[u] = mfma<SAE_KV_BF16>(widen(f.k[u][i][0], f.k[u][i][1]), q[2 * i], s[u]);
-                        s[u] = mfma<SAE_KV_BF16>(widen(f.k[u][i][2], f.k[u][i][3]), q[2 * i + 1], s[u]);
+                        s[u] = mfma16<F16>(widen8(f.k[u][i][0], f.k[u][i][1], 1.0f), q[2 * i], s[u]);
+                        s[u] = mfma16<F16>(widen8(f.k[u][i][2], f.k[u][i][3], 1.0f), q[2 * i + 1], s[u]);
                     } else {
-                        s[u] = mfma<TYPE>(f.k[u][i], q[i], s[u]);
+                        s[u] = mfma16<F16>(f.k[u][i], q[i], s[u]);
                     }
                 }
             }
@@ -307,7 +257,7 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 w[e] = s[e / 4][e % 4] * sl;
-                if constexpr (FP8) w[e] *= __uint_as_float(((f.ks[e / 4] >> (8 * (e % 4))) & 0xFFu) << 23);
+                if constexpr (FP8) w[e] *= scale_of(f.ks[e / 4], e % 4);
             }
             if (!v0 || !v1 || t0 < lo || t0 + STEP > len) {  // uniform: some key of the step is not seen
                 const bool there = vpage ? v1 : v0;
@@ -346,7 +296,7 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
             top = max_groups(top);
             if (__any(top > m)) {  // a head's maximum grew: what is summed so far shrinks
                 const float mn = fmaxf(m, top);
-                const float f0 = mn == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+                const float f0 = mn == NEG_INF ? 0.0f : exp2_(m - mn);
                 m = mn;
                 l *= f0;
 #pragma unroll
@@ -356,25 +306,24 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
             u32x4 hi, lo_;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                w[e] = __builtin_amdgcn_exp2f(w[e] - mu);
+                w[e] = exp2_(w[e] - mu);
                 l += w[e];
-                if constexpr (FP8) w[e] *= __uint_as_float(((f.vs[e / 4] >> (8 * (e % 4))) & 0xFFu) << 23);
+                if constexpr (FP8) w[e] *= scale_of(f.vs[e / 4], e % 4);
             }
             // the weights as two 16-bit numbers each: the product with the values
             // costs twice the (idle) matrix units and keeps 16 bits or more of them
-            constexpr int PT = TYPE == SAE_KV_F16 ? SAE_KV_F16 : SAE_KV_BF16;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 uint32_t h_, l_;
-                split2<PT>(w[2 * e], w[2 * e + 1], h_, l_);
+                split2<F16>(w[2 * e], w[2 * e + 1], h_, l_);
                 hi[e] = h_;
                 lo_[e] = l_;
             }
 #pragma unroll
             for (int i = 0; i < NO; ++i) {
-                const u32x4 v = FP8 ? widen(f.v[i / 2][i % 2 * 2], f.v[i / 2][i % 2 * 2 + 1]) : f.v[FP8 ? 0 : i];
-                o[i] = mfma<PT>(v, hi, o[i]);
-                o[i] = mfma<PT>(v, lo_, o[i]);
+                const u32x4 v = FP8 ? widen8(f.v[i / 2][i % 2 * 2], f.v[i / 2][i % 2 * 2 + 1], 1.0f) : f.v[FP8 ? 0 : i];
+                o[i] = mfma16<F16>(v, hi, o[i]);
+                o[i] = mfma16<F16>(v, lo_, o[i]);
             }
         };
         // the next step's loads are in flight while one is computed
@@ -412,26 +361,17 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
             float z = 0.0f;
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                const float f = mx[w][h] == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(mx[w][h] - top);
+                const float f = mx[w][h] == NEG_INF ? 0.0f : exp2_(mx[w][h] - top);
                 z += lx[w][h] * f;
                 sum += *reinterpret_cast<const f32x4 *>(&ox[w][h][d]) * f;
             }
             if (whole) {
                 const float inv = z == 0.0f ? 0.0f : 1.0f / z;  // no key, or every score -inf
                 const int64_t to = (int64_t)r * a.out_stride + (int64_t)(head0 + h) * D + d;
-                u32x2 b;
-                if constexpr (TYPE == SAE_KV_F16) {
-                    _Float16 y[4] = {(_Float16)(sum[0] * inv), (_Float16)(sum[1] * inv), (_Float16)(sum[2] * inv),
-                                     (_Float16)(sum[3] * inv)};
-                    __builtin_memcpy(&b, y, 8);
-                } else {
-                    __bf16 y[4] = {(__bf16)(sum[0] * inv), (__bf16)(sum[1] * inv), (__bf16)(sum[2] * inv),
-                                   (__bf16)(sum[3] * inv)};
-                    __builtin_memcpy(&b, y, 8);
-                }
-                *reinterpret_cast<u32x2 *>(static_cast<char *>(a.out) + to * 2) = b;
+                *reinterpret_cast<u32x2 *>(static_cast<char *>(a.out) + to * 2) =
+                    u32x2{pack2<F16>(sum[0] * inv, sum[1] * inv), pack2<F16>(sum[2] * inv, sum[3] * inv)};
                 if (a.lse && d == 0)
-                    a.lse[(int64_t)r * a.heads + head0 + h] = z == 0.0f ? NEG_INF : (top + __builtin_amdgcn_logf(z)) * LN2;
+                    a.lse[(int64_t)r * a.heads + head0 + h] = z == 0.0f ? NEG_INF : (top + log2_(z)) * LN2;
             } else {
                 *reinterpret_cast<f32x4 *>(po + h * D + d) = sum;
                 if (d == 0) {
@@ -473,7 +413,7 @@ __global__ void __launch_bounds__(THREADS) k_decode_join(KvDev c, AttnArgs a, Sh
         const float mi = pm[h], zi = pm[COLS + h];
         const f32x4 oi = *reinterpret_cast<const f32x4 *>(pm + 2 * COLS + h * D + d * 4);
         const float top = fmaxf(m, mi), mu = top == NEG_INF ? 0.0f : top;
-        const float fo = __builtin_amdgcn_exp2f(m - mu), fi = __builtin_amdgcn_exp2f(mi - mu);
+        const float fo = exp2_(m - mu), fi = exp2_(mi - mu);
         o = o * fo + oi * fi;
         z = z * fo + zi * fi;
         m = top;
@@ -493,23 +433,16 @@ __global__ void __launch_bounds__(THREADS) k_decode_join(KvDev c, AttnArgs a, Sh
     o = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < JR; ++i) {
-        const float f = __builtin_amdgcn_exp2f(mz[i] - mu);
+        const float f = exp2_(mz[i] - mu);
         z += zz[i] * f;
         o += oz[i][d] * f;
     }
     const float inv = z == 0.0f ? 0.0f : 1.0f / z;
     const int64_t to = (int64_t)p.seq * a.out_stride + (int64_t)head * D + d * 4;
-    u32x2 b;
-    if constexpr (TYPE == SAE_KV_F16) {
-        _Float16 y[4] = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
-        __builtin_memcpy(&b, y, 8);
-    } else {
-        __bf16 y[4] = {(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv), (__bf16)(o[3] * inv)};
-        __builtin_memcpy(&b, y, 8);
-    }
-    *reinterpret_cast<u32x2 *>(static_cast<char *>(a.out) + to * 2) = b;
+    *reinterpret_cast<u32x2 *>(static_cast<char *>(a.out) + to * 2) =
+        u32x2{pack2<is_f16(TYPE)>(o[0] * inv, o[1] * inv), pack2<is_f16(TYPE)>(o[2] * inv, o[3] * inv)};
     if (a.lse && d == 0)
-        a.lse[(int64_t)p.seq * a.heads + head] = z == 0.0f ? NEG_INF : (top + __builtin_amdgcn_logf(z)) * LN2;
+        a.lse[(int64_t)p.seq * a.heads + head] = z == 0.0f ? NEG_INF : (top + log2_(z)) * LN2;
 }
 
 Shape shape_of(int heads, int kvh)

@@ -1,5 +1,5 @@
 // The paged key-value cache as the kernels see it: layout, tables and the
-// lookups shared by k_kv.hip and k_attn.hip.
+// lookups shared by k_kv.hip, k_decode.hip and k_prefill.hip.
 #pragma once
 
 #include "sae_internal.h"
@@ -106,7 +106,8 @@ struct AttnArgs {
     int32_t window, heads;
     void *work;
 };
-hipError_t launch_attn(const KvDev &c, const AttnArgs &a, int type, int dim, bool decode, hipStream_t s);
 hipError_t launch_decode(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s);
+hipError_t launch_prefill(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s);
 size_t decode_work_bytes(int heads, int kvh, int dim);
-size_t attn_work_bytes(int n_tokens, int heads, int kvh, int dim);
+size_t prefill_work_bytes(int dim);
+bool prefill_fits(const KvDev &c, int heads);

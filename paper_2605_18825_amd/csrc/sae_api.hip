@@ -630,6 +630,12 @@ sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
     return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, "sae_kv_read");
 }
 
+static size_t attn_work_bytes(int heads, int kvh, int dim)
+{
+    const size_t d = decode_work_bytes(heads, kvh, dim), p = prefill_work_bytes(dim);
+    return d > p ? d : p;
+}
+
 static sae_status attn_heads(const sae_kv *kv, int32_t n_heads)
 {
     if (n_heads < 1 || n_heads > 1024 || n_heads % kv->n_kv_heads != 0)
@@ -645,7 +651,7 @@ sae_status sae_attn_work_size(const sae_kv *kv, const sae_seqs *seqs, int32_t n_
     if (st == SAE_OK) st = attn_heads(kv, n_heads);
     if (st != SAE_OK) return st;
     if (!bytes) return fail(nullptr, SAE_ERR_ARG, "bytes must be non-NULL");
-    *bytes = attn_work_bytes(n_tokens, n_heads, kv->n_kv_heads, kv->head_dim);
+    *bytes = attn_work_bytes(n_heads, kv->n_kv_heads, kv->head_dim);
     return SAE_OK;
 }
 
@@ -667,10 +673,12 @@ static sae_status attn(const char *name, bool decode, const sae_kv *kv, const sa
     if (!msg) msg = rows_args(out, out_stride, row);
     if (msg) return fail(nullptr, SAE_ERR_ARG, msg);
     if (!aligned(lse, 4)) return fail(nullptr, SAE_ERR_ARG, "lse must be 4-byte aligned");
-    if (!work || !aligned(work, 16) || work_bytes < attn_work_bytes(n_tokens, n_heads, kv->n_kv_heads, kv->head_dim))
+    if (!decode && !prefill_fits(d, n_heads))
+        return fail(nullptr, SAE_ERR_ARG, "too many rows for one call: n_tokens * n_heads / 128 + n_seq * n_kv_heads >= 2^23");
+    if (!work || !aligned(work, 16) || work_bytes < attn_work_bytes(n_heads, kv->n_kv_heads, kv->head_dim))
         return fail(nullptr, SAE_ERR_ARG, "work must be 16-byte aligned and hold sae_attn_work_size bytes");
     const AttnArgs a = {q, out, lse, q_stride, out_stride, scale, window, n_heads, work};
-    hipError_t e = launch_attn(d, a, kv->type, kv->head_dim, decode, s);
+    hipError_t e = (decode ? launch_decode : launch_prefill)(d, a, kv->type, kv->head_dim, s);
     return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, name);
 }
 

@@ -316,3 +316,67 @@ def test_same_call_same_bits():
             (api.sae_attn_decode if qs is None else api.sae_attn_prefill)(kv, seqs, q, o, 0.1, work)
         torch.cuda.synchronize()
         assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("what", [np.nan, np.inf])
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("ty", TYPES)
+def test_values_that_are_not_finite_reach_only_rows_that_see_them(ty, window, what):
+    """Values of NaN or infinity at a few keys of a prompt: earlier rows (and rows past the window) are as without them."""
+    heads, kvh, dim = 4, 2, 128
+    rng = np.random.default_rng(40)
+    lens, new = np.array([150, 90]), np.array([110, 90])
+    ids, inst, bpi, _ = tables(lens, 1, rng)
+    c = Cache(ty, 1, bpi, kvh, dim, rng)
+    size = 1 if ty == O.FP8 else 2
+    bits = {(O.BF16, True): 0x7FC0, (O.BF16, False): 0x7F80, (O.F16, True): 0x7E00, (O.F16, False): 0x7C00}
+    page = O.unpack(c.pages[1], dim, size, 1)
+    for r, t, d in ((0, 77, 5), (0, 100, 64), (1, 89, 127), (1, 31, 0)):
+        where = (ids[r, t // 16], 1, t % 16, d)
+        page[where] = 0x7F if ty == O.FP8 else bits[ty, bool(np.isnan(what))]
+        c.values[1][where] = np.nan if ty == O.FP8 else what
+    c.pages[1] = O.pack(page, size, 1)
+    kv = c.device()
+    starts = np.array([0, 110, 200])
+    dtype = O.BF16 if ty == O.FP8 else ty
+    qval, qbits = to16(rng.standard_normal((200, heads, dim)), dtype)
+    q = torch.as_tensor(qbits).view(DT[dtype]).cuda()
+    out, lse = torch.zeros_like(q), torch.zeros((200, heads), device="cuda")
+    seqs = api.make_seqs(dev32(ids), dev32(lens), q_start=dev32(starts))
+    work = torch.empty(api.sae_attn_work_size(kv, seqs, 200, heads), dtype=torch.uint8, device="cuda")
+    say("values not finite, type %d window %d" % (ty, window))
+    api.sae_attn_prefill(kv, seqs, q, out, 0.1, work, window=window, lse=lse)
+    want, wl, mag, big = oracle_attention(c, ids, inst, lens, starts, qval, 0.1, window)
+    got = out.double().cpu().numpy()
+    fine = np.isfinite(want)
+    assert 0 < (~fine).sum() < 0.05 * fine.size
+    assert np.array_equal(fine, np.isfinite(got))
+    tol, tol_l = O.bounds(np.where(fine, want, 0), wl, np.where(fine, mag, 0), big, dim, dtype)
+    assert np.all(np.abs(got - np.where(fine, want, 0))[fine] <= tol[fine])
+    assert np.all(np.abs(lse.double().cpu().numpy() - wl) <= tol_l)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.125])
+def test_scale_of_zero_and_below(scale):
+    for new in (None, [3, 60, 70]):
+        run(O.BF16, 8, 2, 128, [3, 60, 200], new=new, seed=41, scale=scale)
+
+
+def test_prefill_one_token_each():
+    """Without q_start: one new token per sequence, also where its heads fill several tiles."""
+    rng = np.random.default_rng(42)
+    lens = np.array([1, 33, 0, 500])
+    for heads, kvh in ((8, 2), (300, 1)):
+        ids, inst, bpi, _ = tables(lens, 1, rng)
+        c = Cache(O.BF16, 1, bpi, kvh, 64, rng)
+        kv = c.device()
+        qval, qbits = to16(rng.standard_normal((4, heads, 64)), O.BF16)
+        q = torch.as_tensor(qbits).view(torch.bfloat16).cuda()
+        seqs = api.make_seqs(dev32(ids), dev32(lens))
+        work = torch.empty(api.sae_attn_work_size(kv, seqs, 4, heads), dtype=torch.uint8, device="cuda")
+        want, wl, mag, big = oracle_attention(c, ids, inst, lens, np.arange(5), qval, 0.1, 0)
+        tol, _ = O.bounds(want, wl, mag, big, 64, O.BF16)
+        for call in (api.sae_attn_prefill, api.sae_attn_decode):
+            out = torch.full_like(q, 7.0)
+            call(kv, seqs, q, out, 0.1, work)
+            assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol)
