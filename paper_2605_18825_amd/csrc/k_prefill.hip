@@ -27,18 +27,28 @@ namespace {
 using namespace attn;
 
 constexpr int ROWS = 32;   // rows of a wave
-constexpr int KEYS = 64;   // keys of a step
-constexpr int PAGES = KEYS / SAE_KV_BLOCK;
-constexpr int MIN_SPLIT = 4;     // steps of a split at least
+// Keys of a step: 64, or 32 where a row's state and a step's scores would not fit
+// the registers together.
+constexpr int keys_of(int dim) { return dim == 256 ? 32 : 64; }
+constexpr int MIN_SPLIT = 256;   // keys of a split at least
 constexpr int GROUPS = 512;      // workgroups wanted: two per compute unit
+constexpr int BATCH = 4;         // LDS reads that are in flight while as many products are taken
 constexpr float SLACK = 8.0f;    // of the running maximum, in powers of two
 
-// Orders LDS only: loads from memory stay in flight across it.
+// Everything written to LDS before it, by stores or by to_lds(), is whole after it.
 __device__ __forceinline__ void barrier()
 {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): to_lds() has arrived
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// 16 bytes per lane from memory to LDS, lane l's to `to` + 16 l.
+__device__ __forceinline__ void to_lds(const char *from, char *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
 }
 
 struct Plan {
@@ -55,12 +65,12 @@ struct Tile {
     int rows;              // rows of the tile that there are
     int pos0;              // position of its first new token (may be negative)
     int len;
-    int step0, steps;      // steps of KEYS keys the tile sees: step0 .. step0 + steps - 1
+    int step0, steps;      // steps of keys_of(dim) keys the tile sees: step0 .. step0 + steps - 1
     int parts;             // workgroups they are divided over
     bool none;
 };
 
-__device__ __forceinline__ Tile tile_of(const KvDev &c, const AttnArgs &a, int64_t tile, int rows, int splits)
+__device__ __forceinline__ Tile tile_of(const KvDev &c, const AttnArgs &a, int64_t tile, int rows, int splits, int keys)
 {
     Tile t;
     const int G = a.heads / c.kvh;
@@ -98,24 +108,24 @@ __device__ __forceinline__ Tile tile_of(const KvDev &c, const AttnArgs &a, int64
     const int p0 = t.pos0 + t.token0, p1 = t.pos0 + t.token0 + (t.head0 + t.rows - 1) / G;  // first and last position
     const int lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0;
     if (p1 >= 0) {
-        t.step0 = lo / KEYS;
-        t.steps = p1 / KEYS + 1 - t.step0;
+        t.step0 = lo / keys;
+        t.steps = p1 / keys + 1 - t.step0;
     }
-    t.parts = min(splits, max(1, t.steps / MIN_SPLIT));
+    t.parts = min(splits, max(1, t.steps / (MIN_SPLIT / keys)));
     return t;
 }
 
-// A step's keys and values on their way from the cache to LDS: 16-byte pieces
-// of a thread, unit i of the wave's 1 KiB units.
+// A step's keys or values on their way from the cache to LDS: 16-byte pieces of
+// a thread, unit i of the wave's 1 KiB units.
 template <int TYPE, int D, int NW>
 struct Stage {
     static constexpr bool FP8 = TYPE == SAE_KV_FP8;
     static constexpr int PAGE = SAE_KV_BLOCK * D * (FP8 ? 1 : 2);  // bytes in the cache
-    static constexpr int UNITS = PAGES * PAGE / 1024 / NW;         // units of a wave, of keys and of values each
+    static constexpr int UNITS = keys_of(D) / SAE_KV_BLOCK * PAGE / 1024 / NW;         // units of a wave
     static constexpr int PER_PAGE = PAGE / 1024;
     static_assert(UNITS >= 1, "every wave moves something");
-    u32x4 k[UNITS], v[UNITS];
-    uint32_t ks[UNITS], vs[UNITS][2];
+    u32x4 x[UNITS];
+    uint32_t s[UNITS][2];  // scale bytes of an 8-bit cache
 };
 
 // The wave's rows over steps s0 .. s1 - 1 once more, one key at a time on the
@@ -126,7 +136,7 @@ __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, int64_t b
                      int head, int lo, int pos, f32x16 (&o)[D / 32], float &m, float &l)
 {
     constexpr bool FP8 = TYPE == SAE_KV_FP8, F16 = is_f16(TYPE);
-    constexpr int E = FP8 ? 1 : 2, PAGE = SAE_KV_BLOCK * D * E, ND = FP8 ? 2 : 1;
+    constexpr int E = FP8 ? 1 : 2, PAGE = SAE_KV_BLOCK * D * E, ND = FP8 ? 2 : 1, KEYS = keys_of(D);
     const int h = (int)__lane_id() >> 5;
     const uint16_t *q = static_cast<const uint16_t *>(a.q) + (int64_t)(t.first + token) * a.q_stride + (int64_t)head * D;
     m = NEG_INF;
@@ -181,10 +191,13 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
 {
     constexpr bool FP8 = TYPE == SAE_KV_FP8, F16 = is_f16(TYPE);
     constexpr int PB = SAE_KV_BLOCK * D * 2;  // bytes of a page in LDS
+    constexpr int KEYS = keys_of(D), PAGES = KEYS / SAE_KV_BLOCK, KT = KEYS / 32;
     constexpr int NM = D / 16, NB = D / 32;
     typedef Stage<TYPE, D, NW> St;
-    __shared__ __align__(16) char lds_k[2][PAGES * PB];
-    __shared__ __align__(16) char lds_v[2][PAGES * PB];
+    // arrays of their own: the compiler then sees that a read of one does not depend
+    // on loads into another
+    __shared__ __align__(16) char k_even[PAGES * PB], k_odd[PAGES * PB], v_even[PAGES * PB], v_odd[PAGES * PB];
+    char *const lds_k[2] = {k_even, k_odd}, *const lds_v[2] = {v_even, v_odd};
 
     // blocks go round-robin over the XCDs: the key-value head varies fastest, so
     // that the tiles that read the same keys tend to share an L2; long tiles
@@ -192,7 +205,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     const int per = c.kvh * plan.splits;
     const int64_t tile = plan.tiles - 1 - (int64_t)(blockIdx.x / per);
     const int part = blockIdx.x % per / c.kvh, kvhead = blockIdx.x % c.kvh;
-    const Tile t = tile_of(c, a, tile, NW * ROWS, plan.splits);
+    const Tile t = tile_of(c, a, tile, NW * ROWS, plan.splits, keys_of(D));
     if (t.none || part >= t.parts) return;
     const int G = a.heads / c.kvh;
     const int lane = (int)__lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / SAE_WAVE);
@@ -213,7 +226,6 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     const int wp0 = wrow < t.rows ? t.pos0 + t.token0 + (t.head0 + wrow) / G : -1;
     const int wp1 = wrow < t.rows ? t.pos0 + t.token0 + (t.head0 + min(wrow + ROWS, t.rows) - 1) / G : -1;
     const int wlo1 = a.window > 0 ? max(0, wp1 - a.window + 1) : 0;  // the last row's first key
-    const int wlo0 = a.window > 0 ? max(0, wp0 - a.window + 1) : 0;
 
     const float sl = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * LOG2E;
     u32x4 q[NM];
@@ -245,127 +257,152 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         if (ids >= c.bpi) kv::report(c);
         if (base < 0 || ids >= c.bpi) ids = -1;
     };
-    St st;
-    auto load = [&](int step) {
-        if (step >= s1) return;
-        if (step >= ids_from + SAE_WAVE / PAGES) fetch_ids(step);
+    // bit p: page p of the step has no block
+    auto holes_of = [&](int step) {
+        return (uint32_t)(__ballot(ids < 0) >> ((step - ids_from) * PAGES)) & ((1u << PAGES) - 1);
+    };
+    // the cache block and place of the wave's unit i of a step
+    auto unit_block = [&](int step, int i, int &sub) {
+        const int unit = wave * St::UNITS + i;
+        sub = unit % St::PER_PAGE;
+        const int id = __builtin_amdgcn_readlane(ids, (step - ids_from) * PAGES + unit / St::PER_PAGE);
+        return id < 0 ? 0 : base + id;
+    };
+    // Value pieces (16 bytes: half h of dimension n of 32) lie in LDS at piece 2 n + h
+    // with its lowest bit flipped by bit 4: the lanes that LDS serves together then
+    // read all banks (without the flip two of them met in each).
+    const int flip = lane ^ (lane >> 4 & 1);
+    // A step's keys or values into LDS: 16-bit ones go there directly, 8-bit ones
+    // through registers.  What is there is whole after the next barrier().
+    auto load_k1 = [&](int step, St &st, char *to, int i) __attribute__((always_inline)) {
+        int sub;
+        const int64_t blk = unit_block(step, i, sub);
+        const char *from = c.k + (blk * c.block_bytes + (int64_t)kvhead * St::PAGE + sub * 1024) + (uint32_t)lane * 16u;
+        if constexpr (FP8) {
+            st.x[i] = *reinterpret_cast<const u32x4 *>(from);
+            st.s[i][0] = c.ks[blk * c.scale_stride + kvhead * SAE_KV_BLOCK + (lane & 15)];
+        } else {
+            to_lds(from, to + (wave * St::UNITS + i) * 1024);
+        }
+    };
+    auto load_v1 = [&](int step, St &st, char *to, int i) __attribute__((always_inline)) {
+        int sub;
+        const int64_t blk = unit_block(step, i, sub);
+        const char *from = c.v + (blk * c.block_bytes + (int64_t)kvhead * St::PAGE + sub * 1024);
+        if constexpr (FP8) {
+            st.x[i] = *reinterpret_cast<const u32x4 *>(from + (uint32_t)lane * 16u);
+            const uint8_t *sc = c.vs + blk * c.scale_stride + kvhead * SAE_KV_BLOCK + (lane & 1) * 4;
+            st.s[i][0] = *reinterpret_cast<const uint32_t *>(sc);
+            st.s[i][1] = *reinterpret_cast<const uint32_t *>(sc + 8);
+        } else {
+            to_lds(from + (uint32_t)flip * 16u, to + (wave * St::UNITS + i) * 1024);
+        }
+    };
+    auto load_k = [&](int step, St &st, char *to) {
 #pragma unroll
-        for (int i = 0; i < St::UNITS; ++i) {
-            const int unit = wave * St::UNITS + i, p = unit / St::PER_PAGE;
-            const int id = __builtin_amdgcn_readlane(ids, (step - ids_from) * PAGES + p);
-            const int64_t blk = id < 0 ? 0 : base + id;
-            const int64_t at = blk * c.block_bytes + (int64_t)kvhead * St::PAGE + unit % St::PER_PAGE * 1024 + lane * 16;
-            st.k[i] = *reinterpret_cast<const u32x4 *>(c.k + at);
-            st.v[i] = *reinterpret_cast<const u32x4 *>(c.v + at);
-            if constexpr (FP8) {
-                const int64_t sc = blk * c.scale_stride + kvhead * SAE_KV_BLOCK;
-                st.ks[i] = c.ks[sc + (lane & 15)];
-                st.vs[i][0] = *reinterpret_cast<const uint32_t *>(c.vs + sc + (lane & 1) * 4);
-                st.vs[i][1] = *reinterpret_cast<const uint32_t *>(c.vs + sc + (lane & 1) * 4 + 8);
+        for (int i = 0; i < St::UNITS; ++i) load_k1(step, st, to, i);
+    };
+    auto load_v = [&](int step, St &st, char *to) {
+#pragma unroll
+        for (int i = 0; i < St::UNITS; ++i) load_v1(step, st, to, i);
+    };
+    auto store_k = [&](const St &st, char *lds) {
+        if constexpr (FP8) {
+#pragma unroll
+            for (int i = 0; i < St::UNITS; ++i) {  // 16 dimensions of token lane % 16
+                const int unit = wave * St::UNITS + i, p = unit / St::PER_PAGE, sub = unit % St::PER_PAGE;
+                char *to = lds + p * PB + (sub * 4 + (lane >> 4)) * 512 + (lane & 15) * 16;
+                const float ks = scale_of(st.s[i][0], 0);
+                *reinterpret_cast<u32x4 *>(to) = widen8(st.x[i][0], st.x[i][1], ks);
+                *reinterpret_cast<u32x4 *>(to + 256) = widen8(st.x[i][2], st.x[i][3], ks);
             }
         }
     };
-    // Stage -> LDS buffer; what is past the sequence's end or has no block becomes
-    // zeros in the values (it may be NaN); such keys' scores are masked later.
-    auto store = [&](int step, int buf) {
-        if (step >= s1) return;
+    auto store_v = [&](const St &st, char *lds) {
+        if constexpr (FP8) {
 #pragma unroll
-        for (int i = 0; i < St::UNITS; ++i) {
-            const int unit = wave * St::UNITS + i, p = unit / St::PER_PAGE, sub = unit % St::PER_PAGE;
-            const int id = __builtin_amdgcn_readlane(ids, (step - ids_from) * PAGES + p);
-            const int t0 = step * KEYS + p * SAE_KV_BLOCK;
-            // bit j: token j of a value piece's 8 is there
-            uint32_t keep = 0xFF;
-            if (id < 0 || t0 + SAE_KV_BLOCK > t.len) {  // uniform
-                keep = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (id >= 0 && t0 + (lane & 1) * 4 + (j >> 2) * 8 + (j & 3) < t.len) keep |= 1u << j;
-            }
-            if constexpr (FP8) {
-                // keys: 16 dimensions of token lane % 16; values: 8 tokens of two dimensions
-                char *to = lds_k[buf] + p * PB + (sub * 4 + (lane >> 4)) * 512 + (lane & 15) * 16;
-                const float ks = scale_of(st.ks[i], 0);
-                *reinterpret_cast<u32x4 *>(to) = widen8(st.k[i][0], st.k[i][1], ks);
-                *reinterpret_cast<u32x4 *>(to + 256) = widen8(st.k[i][2], st.k[i][3], ks);
-                char *tv = lds_v[buf] + p * PB + (sub * 2 + (lane >> 5)) * 1024 + (lane >> 1 & 15) * 32 + (lane & 1) * 16;
+            for (int i = 0; i < St::UNITS; ++i) {  // 8 tokens of two dimensions
+                const int unit = wave * St::UNITS + i, p = unit / St::PER_PAGE, sub = unit % St::PER_PAGE;
 #pragma unroll
                 for (int dd = 0; dd < 2; ++dd) {
                     u32x4 w;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {  // tokens 2 j, 2 j + 1 of the piece
-                        const uint32_t x = st.v[i][dd * 2 + j / 2] >> (16 * (j & 1));
-                        float f0 = __builtin_amdgcn_cvt_f32_fp8((int)x, 0) * scale_of(st.vs[i][j / 2], 2 * (j & 1));
-                        float f1 = __builtin_amdgcn_cvt_f32_fp8((int)x, 1) * scale_of(st.vs[i][j / 2], 2 * (j & 1) + 1);
-                        if (!(keep >> (2 * j) & 1)) f0 = 0.0f;
-                        if (!(keep >> (2 * j + 1) & 1)) f1 = 0.0f;
-                        w[j] = pack2<false>(f0, f1);
+                        const uint32_t x = st.x[i][dd * 2 + j / 2] >> (16 * (j & 1));
+                        w[j] = pack2<false>(__builtin_amdgcn_cvt_f32_fp8((int)x, 0) * scale_of(st.s[i][j / 2], 2 * (j & 1)),
+                                            __builtin_amdgcn_cvt_f32_fp8((int)x, 1) * scale_of(st.s[i][j / 2], 2 * (j & 1) + 1));
                     }
-                    *reinterpret_cast<u32x4 *>(tv + dd * 512) = w;
+                    *reinterpret_cast<u32x4 *>(lds + p * PB + (sub * 2 + (lane >> 5)) * 1024 + dd * 512 + (flip & 31) * 16) = w;
                 }
-            } else {
-                const int to = p * PB + sub * 1024 + lane * 16;
-                u32x4 w = st.v[i];
-                if (keep != 0xFF) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        w[j] &= (keep >> (2 * j) & 1 ? 0xFFFFu : 0u) | (keep >> (2 * j + 1) & 1 ? 0xFFFF0000u : 0u);
-                }
-                *reinterpret_cast<u32x4 *>(lds_k[buf] + to) = st.k[i];
-                *reinterpret_cast<u32x4 *>(lds_v[buf] + to) = w;
             }
         }
     };
-
-    auto compute = [&](int step, int buf, uint32_t holes) {
-        const int t0 = step * KEYS;
-        if (t0 > wp1 || t0 + KEYS <= wlo0) return;  // no row of the wave sees a key of the step
-        f32x16 s[2];
+    // Zeros in the values of keys past the sequence's end or without a block (they
+    // may be NaN; their scores are masked).  The whole workgroup, or none of it.
+    auto clean_v = [&](int step, uint32_t holes, char *lds) {
+        if (holes == 0 && (step + 1) * KEYS <= t.len) return;
+        for (int i = threadIdx.x; i < PAGES * PB / 16; i += NW * SAE_WAVE) {
+            const int p = i / (PB / 16), piece = i % 64 ^ (i >> 4 & 1);
+            u32x4 w = *reinterpret_cast<u32x4 *>(lds + i * 16);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+            for (int j = 0; j < 8; ++j) {  // token j of the piece's 8
+                const int key = step * KEYS + p * SAE_KV_BLOCK + (piece & 1) * 4 + (j >> 2) * 8 + (j & 3);
+                if (key >= t.len || (holes >> p & 1)) w[j / 2] &= j & 1 ? 0xFFFFu : 0xFFFF0000u;
+            }
+            *reinterpret_cast<u32x4 *>(lds + i * 16) = w;
+        }
+        barrier();
+    };
+
+    const int kfrag = (n >> 4) * PB + h * 256 + (n & 15) * 16, vfrag = ((n * 2 + h) ^ (n >> 3 & 1)) * 16;
+    auto scores = [&](f32x16 (&s)[KT], int buf) {
+        const char *kp = lds_k[buf] + kfrag;
+#pragma unroll
+        for (int u = 0; u < KT; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
-            const char *kp = lds_k[buf] + (u * 2 + (n >> 4)) * PB + h * 256 + (n & 15) * 16;
 #pragma unroll
-            for (int i = 0; i < NM; ++i) s[u] = mfma32<F16>(*reinterpret_cast<const u32x4 *>(kp + i * 512), q[i], s[u]);
-        }
-        const bool masked = holes != 0 || !full_rows || t0 + KEYS - 1 > wp0 || t0 < wlo1;  // uniform
-        if (masked) {
+        for (int i = 0; i < NM; ++i)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < KT; ++u)
+                s[u] = mfma32<F16>(*reinterpret_cast<const u32x4 *>(kp + u * 2 * PB + i * 512), q[i], s[u]);
+    };
+    auto mask = [&](f32x16 (&s)[KT], int step, uint32_t holes) {
+        const int t0 = step * KEYS;
+        if (holes == 0 && full_rows && t0 + KEYS - 1 <= wp0 && t0 >= wlo1) return;  // uniform
+        asm volatile("");  // a branch: the comparisons are not worth taking on every step
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int p = u * 2 + i / 8;
-                    const int key = t0 + p * SAE_KV_BLOCK + (i / 4 % 2) * 8 + h * 4 + i % 4;
-                    if (key < lo || key > pos) s[u][i] = NEG_INF;
-                }
-            if (holes) {
+        for (int u = 0; u < KT; ++u)
 #pragma unroll
-                for (int p = 0; p < PAGES; ++p)
-                    if (holes >> p & 1) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) s[p / 2][p % 2 * 8 + i] = NEG_INF;
-                    }
+            for (int i = 0; i < 16; ++i) {
+                const int p = u * 2 + i / 8;
+                const int key = t0 + p * SAE_KV_BLOCK + (i / 4 % 2) * 8 + h * 4 + i % 4;
+                if (key < lo || key > pos || (holes >> p & 1)) s[u][i] = NEG_INF;
             }
-        }
+    };
+    // The maximum of a step's scores, in powers of two.
+    auto maximum = [&](const f32x16 (&s)[KT]) {
         float top = s[0][0];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < KT; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
-        top = max_halves(top) * sl;
-        if (__any(top > m + SLACK)) {
-            const float mn = fmaxf(m, top);
-            const float f = mn == NEG_INF ? 0.0f : exp2_(m - mn);
-            m = mn;
-            l *= f;
+        return max_halves(top) * sl;
+    };
+    // Follows the maximum: outputs and sums shrink where it grew by more than SLACK.
+    auto follow = [&](float top) {
+        if (!__any(top > m + SLACK)) return;
+        const float mn = fmaxf(m, top);
+        const float f = mn == NEG_INF ? 0.0f : exp2_(m - mn);
+        m = mn;
+        l *= f;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) o[b] *= f;
-        }
+        for (int b = 0; b < NB; ++b) o[b] *= f;
+    };
+    auto weights = [&](const f32x16 (&s)[KT], u32x4 (&w)[PAGES]) {
         const float mu = m == NEG_INF ? 0.0f : -m;
-        u32x4 w[PAGES];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < KT; ++u)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 const float x = exp2_(__builtin_fmaf(s[u][i], sl, mu)), y = exp2_(__builtin_fmaf(s[u][i + 1], sl, mu));
@@ -373,32 +410,144 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
                 l += y;
                 w[u * 2 + i / 8][i / 2 % 4] = pack2<F16>(x, y);
             }
-        const char *vp = lds_v[buf] + n * 32 + h * 16;
+    };
+    auto outputs = [&](const u32x4 (&w)[PAGES], int buf) {
+        const char *vp = lds_v[buf] + vfrag;
 #pragma unroll
         for (int p = 0; p < PAGES; ++p)
 #pragma unroll
             for (int b = 0; b < NB; ++b)
                 o[b] = mfma32<F16>(*reinterpret_cast<const u32x4 *>(vp + p * PB + b * 1024), w[p], o[b]);
     };
-    // bit p: page p of the step has no block
-    auto holes_of = [&](int step) {
-        return (uint32_t)(__ballot(ids < 0) >> ((step - ids_from) * PAGES)) & ((1u << PAGES) - 1);
-    };
 
     if (s0 < s1) {
+        // Step t's weights are computed while the matrix units take step t + 1's
+        // scores, and that step's maximum while they add step t to the outputs: keys
+        // are staged one step ahead of values.
+        St sk, sv;
+        f32x16 s[KT];
+        u32x4 w[PAGES];
         fetch_ids(s0);
-        load(s0);
-        store(s0, 0);
-        uint32_t holes = holes_of(s0);
-        for (int step = s0; step < s1; ++step) {
-            const int buf = (step - s0) & 1;
-            barrier();       // buffer buf is whole; the other one has been read
-            load(step + 1);  // may replace the table entries
-            compute(step, buf, holes);
-            if (step + 1 < s1) {
-                holes = holes_of(step + 1);
-                store(step + 1, buf ^ 1);
+        uint32_t holes0 = holes_of(s0), holes = 0;  // of the step whose values, and of the one whose scores come next
+        {
+            St k0;
+            const int next = min(s0 + 1, s1 - 1);
+            load_k(s0, k0, k_even);
+            load_v(s0, sv, v_even);
+            load_k(next, sk, k_odd);
+            holes = holes_of(next);
+            store_k(k0, k_even);
+            store_v(sv, v_even);
+            store_k(sk, k_odd);
+        }
+        barrier();
+        scores(s, 0);
+        mask(s, s0, holes0);
+        follow(maximum(s));
+        int step = s0;
+        auto body = [&](f32x16 (&s)[KT], f32x16 (&s2)[KT], int buf) __attribute__((always_inline)) {
+            // here: s are this step's scores; its values and the next one's keys are in LDS
+            clean_v(step, holes0, lds_v[buf]);
+            // keys two steps ahead; past the end the last ones again, never used
+            const int ahead = min(step + 2, s1 - 1);
+            if (ahead >= ids_from + SAE_WAVE / PAGES) fetch_ids(step + 1);
+            const uint32_t holes2 = holes_of(ahead);
+            if constexpr (FP8) {
+                load_k(ahead, sk, nullptr);
+                load_v(step + 1, sv, nullptr);
             }
+            // Scores 2 j, 2 j + 1 become weights.  A vector operation costs a product less
+            // than its own time where every product has a few beside it, and more the more
+            // it has: EARLY pairs go with the first products, the others and the maximum
+            // with the second.
+            constexpr int PAIRS = 8 * KT, EARLY = PAIRS * 3 / 4;
+            const float mu = m == NEG_INF ? 0.0f : -m;
+            auto pair = [&](int j) __attribute__((always_inline)) {
+                const float x = exp2_(__builtin_fmaf(s[j / 8][j % 8 * 2], sl, mu));
+                const float y = exp2_(__builtin_fmaf(s[j / 8][j % 8 * 2 + 1], sl, mu));
+                l += x;
+                l += y;
+                uint32_t z = pack2<F16>(x, y);
+                asm volatile("" : "+v"(z), "+v"(l));  // here, not where it is used
+                w[j / 4][j % 4] = z;
+            };
+            {
+                // products, LDS reads and vector operations in this order
+                const char *kp = lds_k[buf ^ 1] + kfrag;
+                auto piece = [&](int i) { return *reinterpret_cast<const u32x4 *>(kp + i % KT * 2 * PB + i / KT * 512); };
+                u32x4 f[2 * BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) f[i] = piece(i);
+#pragma unroll
+                for (int u = 0; u < KT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s2[u][i] = 0.0f;
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < NM * KT; ++i) {
+                    if (i % BATCH == 0) {
+#pragma unroll
+                        for (int j = i + BATCH; j < i + 2 * BATCH && j < NM * KT; ++j) f[j % (2 * BATCH)] = piece(j);
+                    }
+                    s2[i % KT] = mfma32<F16>(f[i % (2 * BATCH)], q[i / KT], s2[i % KT]);
+                    if (!FP8 && i * 2 * St::UNITS % (NM * KT) == 0) {  // spread: loads issued at once stall the wave
+                        const int u = i * 2 * St::UNITS / (NM * KT);
+                        if (u < St::UNITS) load_k1(ahead, sk, lds_k[buf], u);
+                        else load_v1(step + 1, sv, lds_v[buf ^ 1], u - St::UNITS);
+                    }
+#pragma unroll
+                    for (int j = i * EARLY / (NM * KT); j < (i + 1) * EARLY / (NM * KT); ++j) pair(j);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            mask(s2, step + 1, holes);
+            float top = s2[0][0];
+            {
+                const char *vp = lds_v[buf] + vfrag;
+                auto piece = [&](int i) { return *reinterpret_cast<const u32x4 *>(vp + i / NB * PB + i % NB * 1024); };
+                u32x4 f[2 * BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) f[i] = piece(i);
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int N = NB * PAGES, LATE = N / 2;  // the last page's weights are first used after 3 N / 4 products
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    if (i % BATCH == 0) {
+#pragma unroll
+                        for (int j = i + BATCH; j < i + 2 * BATCH && j < N; ++j) f[j % (2 * BATCH)] = piece(j);
+                    }
+                    o[i % NB] = mfma32<F16>(f[i % (2 * BATCH)], w[i / NB], o[i % NB]);
+#pragma unroll
+                    for (int j = EARLY + i * (PAIRS - EARLY) / LATE; j < EARLY + (i + 1) * (PAIRS - EARLY) / LATE; ++j)
+                        if (i < LATE) pair(j);
+#pragma unroll
+                    for (int j = (i - LATE / 2) * 16 * KT / (N - LATE / 2); j < (i + 1 - LATE / 2) * 16 * KT / (N - LATE / 2); ++j)
+                        if (i >= LATE / 2) top = fmaxf(top, s2[j / 16][j % 16]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            follow(max_halves(top) * sl);
+            store_k(sk, lds_k[buf]);
+            store_v(sv, lds_v[buf ^ 1]);
+            holes0 = holes;
+            holes = holes2;
+            barrier();  // keys of step + 2 and values of step + 1 are whole, what they replaced was read before
+            ++step;
+        };
+        f32x16 t[KT];
+        while (step + 2 < s1) {
+            body(s, t, 0);
+            body(t, s, 1);
+        }
+        if (step + 1 < s1) {
+            body(s, t, 0);
+            clean_v(step, holes0, v_odd);
+            weights(t, w);
+            outputs(w, 1);
+        } else {
+            clean_v(step, holes0, v_even);
+            weights(s, w);
+            outputs(w, 0);
         }
     }
 
@@ -447,7 +596,7 @@ __global__ void __launch_bounds__(SAE_WAVE) k_prefill_join(KvDev c, AttnArgs a, 
     const int wave = blockIdx.y % NW, b = blockIdx.y / NW;
     const int64_t tile = blockIdx.x / c.kvh;
     const int kvhead = blockIdx.x % c.kvh, G = a.heads / c.kvh;
-    const Tile t = tile_of(c, a, tile, NW * ROWS, plan.splits);
+    const Tile t = tile_of(c, a, tile, NW * ROWS, plan.splits, keys_of(D));
     if (t.none || t.parts == 1) return;
     const int lane = (int)__lane_id(), n = lane & 31, h = lane >> 5;
     const int row = wave * ROWS + n;
