@@ -303,15 +303,22 @@ def _rows(t, heads, dim):
     (a slice of fused rows); its heads and dimensions are contiguous."""
     if not t.is_cuda:
         raise SaeError("expected a device tensor")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+    n, h, d = t.shape if t.dim() == 3 else (0, 0, 0)
+    if h != heads or d != dim:
         raise SaeError("expected a tensor [n][%d][%d], got %s" % (heads, dim, tuple(t.shape)))
-    n, _, _ = t.shape
     s0, s1, s2 = t.stride()
-    if n and (s2 != 1 or (heads > 1 and s1 != dim)):
+    if n and (s2 != 1 or (s1 != dim and heads > 1)):
         raise SaeError("a token's heads must be contiguous")
-    if t.dtype not in _KV_DTYPE:
+    ty = _KV_DTYPE.get(t.dtype)
+    if ty is None:
         raise SaeError("expected bfloat16 or float16")
-    return t.data_ptr(), s0 if n > 1 else heads * dim, _KV_DTYPE[t.dtype]
+    return t.data_ptr(), s0 if n > 1 else heads * dim, ty, n
+
+
+def _raw_stream(t, stream):
+    """The stream's handle; by default the current one of t's device (a decode step is a few microseconds: the handle
+    is taken without making a stream object)."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def make_kv(type, n_instances, blocks_per_instance, n_kv_heads, head_dim, k, v, k_scale=None, v_scale=None, status=None,
@@ -367,11 +374,14 @@ def make_seqs(block_ids, kv_len, q_start=None, inst=None):
 
 
 def _kv_move(fn, kv, seqs, k, v, stream):
-    kp, ks, kt = _rows(k, kv.n_kv_heads, kv.head_dim)
-    vp, vs, vt = _rows(v, kv.n_kv_heads, kv.head_dim)
-    if kt != vt or k.shape[0] != v.shape[0]:
+    heads, dim = kv.n_kv_heads, kv.head_dim
+    kp, ks, kt, n = _rows(k, heads, dim)
+    vp, vs, vt, vn = _rows(v, heads, dim)
+    if kt != vt or n != vn:
         raise SaeError("k and v must have one type and one length")
-    _check(None, fn(ctypes.byref(kv), ctypes.byref(seqs), k.shape[0], kt, kp, ks, vp, vs, _stream(stream)))
+    st = fn(ctypes.byref(kv), ctypes.byref(seqs), n, kt, kp, ks, vp, vs, _raw_stream(k, stream))
+    if st:
+        _check(None, st)
 
 
 def sae_kv_write(kv, seqs, k, v, stream=None):
@@ -392,11 +402,12 @@ def sae_attn_work_size(kv, seqs, n_tokens, n_heads):
     return n.value
 
 
-def _attn_rows(kv, seqs, q, out, lse, work):
-    n, heads = q.shape[0], q.shape[1]
-    qp, qs, qt = _rows(q, heads, kv.head_dim)
-    op, os_, ot = _rows(out, heads, kv.head_dim)
-    if ot != qt or out.shape[0] != n:
+def _attn_rows(kv, q, out, lse, work):
+    dim = kv.head_dim
+    heads = q.shape[1] if q.dim() == 3 else 0
+    qp, qs, qt, n = _rows(q, heads, dim)
+    op, os_, ot, on = _rows(out, heads, dim)
+    if ot != qt or on != n:
         raise SaeError("out must have q's type and shape")
     if lse is not None and (lse.dtype != torch.float32 or lse.numel() != n * heads):
         raise SaeError("lse must be float32 [n][heads]")
@@ -405,18 +416,22 @@ def _attn_rows(kv, seqs, q, out, lse, work):
 
 def sae_attn_decode(kv, seqs, q, out, scale, work, window=0, lse=None, stream=None):
     """Attention of one new token per sequence: q, out [n_seq][heads][head_dim]."""
-    n, heads, ty, qp, qs, op, os_, lp, wp, wn = _attn_rows(kv, seqs, q, out, lse, work)
+    n, heads, ty, qp, qs, op, os_, lp, wp, wn = _attn_rows(kv, q, out, lse, work)
     if n != seqs.n_seq:
         raise SaeError("q must have a row per sequence")
-    _check(None, _lib.load().sae_attn_decode(ctypes.byref(kv), ctypes.byref(seqs), heads, ty, qp, qs, op, os_, lp, scale,
-                                             int(window), wp, wn, _stream(stream)))
+    st = _lib.load().sae_attn_decode(ctypes.byref(kv), ctypes.byref(seqs), heads, ty, qp, qs, op, os_, lp, scale,
+                                     window, wp, wn, _raw_stream(q, stream))
+    if st:
+        _check(None, st)
 
 
 def sae_attn_prefill(kv, seqs, q, out, scale, work, window=0, lse=None, stream=None):
     """Causal attention of the new tokens over their sequences' caches: q, out [n_tokens][heads][head_dim]."""
-    n, heads, ty, qp, qs, op, os_, lp, wp, wn = _attn_rows(kv, seqs, q, out, lse, work)
-    _check(None, _lib.load().sae_attn_prefill(ctypes.byref(kv), ctypes.byref(seqs), n, heads, ty, qp, qs, op, os_, lp,
-                                              scale, int(window), wp, wn, _stream(stream)))
+    n, heads, ty, qp, qs, op, os_, lp, wp, wn = _attn_rows(kv, q, out, lse, work)
+    st = _lib.load().sae_attn_prefill(ctypes.byref(kv), ctypes.byref(seqs), n, heads, ty, qp, qs, op, os_, lp, scale,
+                                      window, wp, wn, _raw_stream(q, stream))
+    if st:
+        _check(None, st)
 
 
 def status_names(bits):

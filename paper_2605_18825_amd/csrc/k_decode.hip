@@ -38,6 +38,9 @@ constexpr int NW = 4, THREADS = NW * SAE_WAVE;
 constexpr int STEP = 32;       // keys a wave takes at a time: two pages
 constexpr int COLS = 16;       // query heads of a tile
 constexpr int MIN_STEPS = NW;  // steps of a workgroup at least (where there are as many)
+constexpr int EXTRA = 8;       // steps that a sequence costs beside its own
+// Bytes of keys and values up to which a sequence is left to one workgroup per head.
+constexpr int64_t SINGLE = 384 << 10;
 constexpr int GROUPS = 512;    // workgroups of a call, about: two per compute unit
 // Two values rounded to the 16-bit type, and what the rounding left, rounded too.
 template <bool F16>
@@ -55,11 +58,16 @@ __device__ __forceinline__ float sum_groups(float x)
 
 // First key and number of steps of a sequence of n tokens (one step, which
 // sees nothing, where there is no key: its workgroup writes the zeros).
-__device__ __forceinline__ int first_key(int n, int window) { return window > 0 && n > window ? n - window : 0; }
+__device__ __forceinline__ int first_key(int n, int window) { return window > 0 ? max(n - window, 0) : 0; }
 __device__ __forceinline__ int steps_of(int n, int window)
 {
     return n <= 0 ? 1 : (n + STEP - 1) / STEP - first_key(n, window) / STEP;
 }
+
+// What a sequence costs its workgroup: its steps and, behind them, as much as EXTRA
+// steps take for its start and end (round trips for its table and first keys, the
+// waves' parts joined).
+__device__ __forceinline__ int cost_of(int n, int window) { return steps_of(n, window) + EXTRA; }
 
 // Steps per workgroup, for `total` steps over `groups` workgroups.
 __device__ __forceinline__ long long steps_per(long long total, int groups)
@@ -71,75 +79,95 @@ __device__ __forceinline__ long long steps_per(long long total, int groups)
 // Where workgroup x of a head starts: its first sequence and the step in it.
 struct Start {
     long long per, begin, end;  // steps begin .. end - 1 of all
-    int seq;
-    long long seq_at;           // number of that sequence's first step
+    int seq, len;               // that sequence and its length
+    long long seq_at;           // number of its first step
 };
 
 // Exclusive scan over the workgroup's threads; total in every thread.
-__device__ __forceinline__ long long scan(long long v, long long &total, long long *lds)
+template <typename T>
+__device__ __forceinline__ T scan(T v, T &total, T *lds)
 {
     const int lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
-    long long s = v;
+    T s = v;
 #pragma unroll
     for (int o = 1; o < SAE_WAVE; o <<= 1) {
-        const long long u = __shfl_up(s, o);
+        const T u = __shfl_up(s, o);
         if (lane >= o) s += u;
     }
     if (lane == SAE_WAVE - 1) lds[wave] = s;
     __syncthreads();
-    long long before = 0;
+    T before = 0;
     total = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
         if (w < wave) before += lds[w];
         total += lds[w];
     }
-    __syncthreads();
     return before + s - v;
 }
 
 __device__ __forceinline__ Start find_start(const KvDev &c, int window, int x, int groups)
 {
     __shared__ long long tmp[NW];
+    __shared__ uint32_t tmp32[NW];
     __shared__ long long found_at;
-    __shared__ int found_seq;
+    __shared__ int found_seq, found_len;
     const int n = c.n_seq, chunk = (n + THREADS - 1) / THREADS;
     const int r0 = min((int)threadIdx.x * chunk, n), r1 = min(r0 + chunk, n);
-    long long sum = 0;
-    for (int r = r0; r < r1; ++r) sum += steps_of(kv::seq_len(c, r), window);
     Start s;
-    long long total;
-    long long at = scan(sum, total, tmp);
+    long long total, at, sum = 0;
+    int len = 0;
+    if (chunk == 1) {  // 32 bits are enough: 256 sequences of 2^23 steps at most
+        if (r0 < n) {
+            len = kv::seq_len(c, r0);
+            sum = cost_of(len, window);
+        }
+        uint32_t t32;
+        at = scan((uint32_t)sum, t32, tmp32);
+        total = t32;
+    } else {
+        for (int r = r0; r < r1; ++r) sum += cost_of(kv::seq_len(c, r), window);
+        at = scan(sum, total, tmp);
+    }
     s.per = steps_per(total, groups);
     s.begin = x * s.per;
     s.end = min(s.begin + s.per, total);
     if (s.begin < total && at <= s.begin && s.begin < at + sum) {  // one thread
         int r = r0;
-        for (;; ++r) {
-            const int k = steps_of(kv::seq_len(c, r), window);
-            if (s.begin < at + k) break;
-            at += k;
-        }
+        if (chunk > 1)
+            for (;; ++r) {
+                len = kv::seq_len(c, r);
+                const int k = cost_of(len, window);
+                if (s.begin < at + k) break;
+                at += k;
+            }
         found_seq = r;
+        found_len = len;
         found_at = at;
     }
     __syncthreads();
-    s.seq = s.begin < total ? found_seq : n;
-    s.seq_at = s.begin < total ? found_at : total;
+    const bool any = s.begin < total;
+    s.seq = __builtin_amdgcn_readfirstlane(any ? found_seq : n);
+    s.len = __builtin_amdgcn_readfirstlane(any ? found_len : 0);
+    s.seq_at = any ? found_at : total;
     return s;
 }
 
-// Workspace: per workgroup x a description of the sequence that begins in it
-// and ends in a later one, then per (x, head tile, slot) 16 maxima, 16 sums and
+// Workspace: descriptions of split sequences, by sequence where there are no more
+// of them than workgroups (the join then has a workgroup for each), else by the
+// workgroup x in which the sequence begins (one at most continues past it); then per (x, head tile, slot) 16 maxima, 16 sums and
 // 16 rows of unnormalised outputs.
 struct Part {
-    int seq, count;  // parts of that sequence: workgroups x .. x + count - 1; seq < 0: none
+    int seq, first, count;  // its parts: workgroups first .. first + count - 1; count < 2: none to join
+    int pad;
 };
 __host__ __device__ constexpr size_t part_floats(int dim) { return (size_t)COLS * (dim + 2); }
 __host__ __device__ constexpr size_t meta_bytes(int groups) { return ((size_t)groups * sizeof(Part) + 15) / 16 * 16; }
 
 struct Shape {
     int groups, tiles, per_kv;  // workgroups per head tile; head tiles in all; head tiles of a key-value head
+    int by_seq;                 // descriptions go by sequence
+    int single;                 // one workgroup per sequence and head tile: none is split
 };
 
 // One step's keys and values of a lane, as loaded.
@@ -168,20 +196,34 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
     const int cols = min(COLS, G - tile % sh.per_kv * COLS);
     const int lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
     const int n = lane & 15, g = lane >> 4;
-    const Start st = find_start(c, a.window, x, sh.groups);
+    Start st;
+    if (sh.single) {
+        st.seq = x;
+        st.len = kv::seq_len(c, x);
+        st.seq_at = st.begin = 0;
+        st.per = st.end = 1ll << 40;
+    } else {
+        st = find_start(c, a.window, x, sh.groups);
+    }
     Part *meta = reinterpret_cast<Part *>(a.work);
     float *parts = reinterpret_cast<float *>(static_cast<char *>(a.work) + meta_bytes(sh.groups));
-    Part mine = {-1, 0};
+    Part mine = {0, 0, 0, 0};
     const float sl = a.scale * LOG2E;
     // the lane's place in a page (bytes)
     const int koff = g * 256 + (lane & 7) * 16, voff = (lane & 15) * 32 + (g & 1) * 16;
     const bool kpage = lane & 8, vpage = lane & 32;
 
     long long at = st.begin, seq_at = st.seq_at;
-    for (int r = st.seq; at < st.end; ++r) {
-        const int len = kv::seq_len(c, r), total = steps_of(len, a.window);
+    for (int r = st.seq, len = st.len, next = 0; at < st.end; ++r, len = kv::checked_len(c, next)) {
+        const int total = steps_of(len, a.window);
+        if (!sh.single) next = c.len[min(r + 1, c.n_seq - 1)];  // on its way while this sequence is taken
         const int lo = first_key(len, a.window);
         const int s0 = (int)(at - seq_at), s1 = (int)min((long long)total, st.end - seq_at);
+        const long long after = seq_at + total + EXTRA;
+        if (s0 >= total) {  // uniform: the workgroup before had its last step
+            at = seq_at = after;
+            continue;
+        }
         const int step0 = lo / STEP;  // in steps of the whole sequence
         const int64_t base = kv::seq_base(c, r);
         u32x4 q[NQ];
@@ -208,9 +250,9 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
             if (ids_from < 0 || j >= ids_from + 32) {  // uniform
                 ids_from = j;
                 const int page = 2 * (step0 + s0 + wave + NW * (j + (lane >> 1))) + (lane & 1);
-                ids = -1;
-                if (j + (lane >> 1) < count && page * SAE_KV_BLOCK < len)
-                    ids = c.ids[(int64_t)r * c.max_blocks + page];
+                // (the first load need not wait for the length)
+                ids = page < c.max_blocks ? c.ids[(int64_t)r * c.max_blocks + page] : -1;
+                if (j + (lane >> 1) >= count || page * SAE_KV_BLOCK >= len) ids = -1;
                 if (ids >= c.bpi) kv::report(c);
                 if (base < 0 || ids >= c.bpi) ids = -1;
             }
@@ -380,42 +422,59 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
                 }
             }
         }
-        if (s0 == 0 && s1 < total) {
-            mine.seq = r;
-            mine.count = (int)((seq_at + total - 1) / st.per) - x + 1;
+        if (sh.single) return;
+        if (s0 == 0) {
+            const Part p = {r, x, (int)((seq_at + total - 1) / st.per) - x + 1, 0};
+            if (sh.by_seq && tile == 0 && threadIdx.x == 0) meta[r] = p;
+            if (p.count > 1) mine = p;
         }
-        at = seq_at + s1;
-        seq_at += total;
+        at = seq_at = after;
     }
-    if (tile == 0 && threadIdx.x == 0) meta[x] = mine;
+    if (!sh.by_seq && tile == 0 && threadIdx.x == 0) meta[x] = mine;
 }
 
-// Joins the parts of the sequence that begins in workgroup x and ends in a
-// later one: one workgroup per (x, query head), its threads in JR rows of D / 4,
-// row i taking parts i, i + JR, ...
+// Joins a split sequence's parts: one workgroup per (description, query head), its
+// threads in JR rows of D / 4, row i taking parts i, i + JR, ..., UN of them at once.
 template <int TYPE, int D>
 __global__ void __launch_bounds__(THREADS) k_decode_join(KvDev c, AttnArgs a, Shape sh)
 {
-    constexpr int LD = D / 4, JR = THREADS / LD;
+    constexpr int LD = D / 4, JR = THREADS / LD, UN = 4;
     __shared__ float mz[JR], zz[JR];
     __shared__ f32x4 oz[JR][LD];
-    const int x = blockIdx.x, head = blockIdx.y;
-    const Part p = reinterpret_cast<const Part *>(a.work)[x];
-    if (p.seq < 0) return;
+    const int head = blockIdx.y;
+    const Part p = reinterpret_cast<const Part *>(a.work)[blockIdx.x];
+    if (p.count < 2) return;
     const float *parts = reinterpret_cast<const float *>(static_cast<const char *>(a.work) + meta_bytes(sh.groups));
     const int G = a.heads / c.kvh, u = head % G;
     const int tile = head / G * sh.per_kv + u / COLS, h = u % COLS;
     const int row = threadIdx.x / LD, d = threadIdx.x % LD;
     float m = NEG_INF, z = 0.0f;
     f32x4 o = {0, 0, 0, 0};
-    for (int i = row; i < p.count; i += JR) {
-        const float *pm = parts + (((size_t)(x + i) * sh.tiles + tile) * 2 + (i == 0 ? 1 : 0)) * part_floats(D);
-        const float mi = pm[h], zi = pm[COLS + h];
-        const f32x4 oi = *reinterpret_cast<const f32x4 *>(pm + 2 * COLS + h * D + d * 4);
-        const float top = fmaxf(m, mi), mu = top == NEG_INF ? 0.0f : top;
-        const float fo = exp2_(m - mu), fi = exp2_(mi - mu);
-        o = o * fo + oi * fi;
-        z = z * fo + zi * fi;
+    for (int i = row; i < p.count; i += JR * UN) {
+        float mi[UN], zi[UN];
+        f32x4 oi[UN];
+#pragma unroll
+        for (int k = 0; k < UN; ++k) {
+            const int j = min(i + k * JR, p.count - 1);  // past the end: weighs nothing below
+            const float *pm = parts + (((size_t)(p.first + j) * sh.tiles + tile) * 2 + (j == 0 ? 1 : 0)) * part_floats(D);
+            mi[k] = pm[h];
+            zi[k] = pm[COLS + h];
+            oi[k] = *reinterpret_cast<const f32x4 *>(pm + 2 * COLS + h * D + d * 4);
+        }
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < UN; ++k)
+            if (i + k * JR < p.count) top = fmaxf(top, mi[k]);
+        const float mu = top == NEG_INF ? 0.0f : top, f = exp2_(m - mu);
+        o *= f;
+        z *= f;
+#pragma unroll
+        for (int k = 0; k < UN; ++k)
+            if (i + k * JR < p.count) {
+                const float fk = exp2_(mi[k] - mu);
+                o += oi[k] * fk;
+                z += zi[k] * fk;
+            }
         m = top;
     }
     if (d == 0) {
@@ -445,24 +504,30 @@ __global__ void __launch_bounds__(THREADS) k_decode_join(KvDev c, AttnArgs a, Sh
         a.lse[(int64_t)p.seq * a.heads + head] = z == 0.0f ? NEG_INF : (top + log2_(z)) * LN2;
 }
 
-Shape shape_of(int heads, int kvh)
+Shape shape_of(int heads, int kvh, int n_seq, int64_t longest = 1ll << 40)
 {
     Shape s;
     s.per_kv = (heads / kvh + COLS - 1) / COLS;
     s.tiles = kvh * s.per_kv;
     s.groups = GROUPS / s.tiles > 1 ? GROUPS / s.tiles : 1;
+    s.by_seq = n_seq <= s.groups;
+    s.single = longest <= SINGLE;
     return s;
 }
 
 template <int TYPE, int D>
 hipError_t launch(const KvDev &c, const AttnArgs &a, hipStream_t s)
 {
-    const Shape sh = shape_of(a.heads, c.kvh);
-    hipLaunchKernelGGL((k_decode<TYPE, D>), dim3(sh.groups, sh.tiles), dim3(THREADS), 0, s, c, a, sh);
+    // bytes of the longest sequence that the table holds (or the window lets be seen), per head
+    int64_t longest = (int64_t)c.max_blocks * SAE_KV_BLOCK;
+    if (a.window > 0 && longest > a.window) longest = a.window;
+    const Shape sh = shape_of(a.heads, c.kvh, c.n_seq, longest * 2 * D * (TYPE == SAE_KV_FP8 ? 1 : 2));
+    hipLaunchKernelGGL((k_decode<TYPE, D>), dim3(sh.single ? c.n_seq : sh.groups, sh.tiles), dim3(THREADS), 0, s, c, a, sh);
     hipError_t e = hipGetLastError();
-    // one workgroup per head: no sequence is split
-    if (e != hipSuccess || sh.groups == 1) return e;
-    hipLaunchKernelGGL((k_decode_join<TYPE, D>), dim3(sh.groups, a.heads), dim3(THREADS), 0, s, c, a, sh);
+    // one workgroup per head or per sequence: none is split
+    if (e != hipSuccess || sh.groups == 1 || sh.single) return e;
+    hipLaunchKernelGGL((k_decode_join<TYPE, D>), dim3(sh.by_seq ? c.n_seq : sh.groups, a.heads), dim3(THREADS),
+                       0, s, c, a, sh);
     return hipGetLastError();
 }
 
@@ -476,7 +541,7 @@ hipError_t launch_dim(const KvDev &c, const AttnArgs &a, int dim, hipStream_t s)
 
 size_t decode_work_bytes(int heads, int kvh, int dim)
 {
-    const Shape s = shape_of(heads, kvh);
+    const Shape s = shape_of(heads, kvh, 0);
     return meta_bytes(s.groups) + (size_t)s.groups * s.tiles * 2 * part_floats(dim) * sizeof(float);
 }
 

@@ -25,10 +25,9 @@ __device__ __forceinline__ void report(const KvDev &c)
     if (c.status) atomicOr(c.status, (uint32_t)SAE_ST_BAD_BLOCK);
 }
 
-// Length of sequence r; one that its table cannot hold is reported and cut.
-__device__ __forceinline__ int seq_len(const KvDev &c, int r)
+// A sequence's length; one that its table cannot hold is reported and cut.
+__device__ __forceinline__ int checked_len(const KvDev &c, int n)
 {
-    const int n = c.len[r];
     const long long most = (long long)c.max_blocks * SAE_KV_BLOCK;
     if (n < 0 || n > most) {
         report(c);
@@ -36,6 +35,8 @@ __device__ __forceinline__ int seq_len(const KvDev &c, int r)
     }
     return n;
 }
+
+__device__ __forceinline__ int seq_len(const KvDev &c, int r) { return checked_len(c, c.len[r]); }
 
 // First pool block of sequence r's instance, or -1.
 __device__ __forceinline__ int64_t seq_base(const KvDev &c, int r)
