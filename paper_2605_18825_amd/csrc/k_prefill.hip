@@ -20,6 +20,8 @@
 //
 // Where tiles are few, each one's keys are split over several workgroups, whose
 // unnormalised outputs k_prefill_join adds in order.
+#include <algorithm>
+
 #include "attn_tile.h"
 
 namespace {
@@ -30,9 +32,9 @@ constexpr int ROWS = 32;   // rows of a wave
 // Keys of a step: 64, or 32 where a row's state and a step's scores would not fit
 // the registers together.
 constexpr int keys_of(int dim) { return dim == 256 ? 32 : 64; }
-constexpr int MIN_SPLIT = 256;   // keys of a split at least
-constexpr int GROUPS = 512;      // workgroups wanted: two per compute unit
-constexpr int BATCH = 4;         // LDS reads that are in flight while as many products are taken
+constexpr int MIN_SPLIT = 128;   // keys of a split at least
+// Workgroups wanted: two per compute unit, one of the larger heads.
+constexpr int groups_of(int dim) { return dim == 256 ? 256 : 512; }
 constexpr float SLACK = 8.0f;    // of the running maximum, in powers of two
 
 // Everything written to LDS before it, by stores or by to_lds(), is whole after it.
@@ -133,11 +135,11 @@ struct Stage {
 // for values that are not finite.  Same state as the loop it replaces.
 template <int TYPE, int D>
 __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, int64_t base, int kvhead, int s0, int s1, int token,
-                     int head, int lo, int pos, f32x16 (&o)[D / 32], float &m, float &l)
+                     int head, int pos, f32x16 (&o)[D / 32], float &m, float &l)
 {
     constexpr bool FP8 = TYPE == SAE_KV_FP8, F16 = is_f16(TYPE);
     constexpr int E = FP8 ? 1 : 2, PAGE = SAE_KV_BLOCK * D * E, ND = FP8 ? 2 : 1, KEYS = keys_of(D);
-    const int h = (int)__lane_id() >> 5;
+    const int h = (int)__lane_id() >> 5, lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
     const uint16_t *q = static_cast<const uint16_t *>(a.q) + (int64_t)(t.first + token) * a.q_stride + (int64_t)head * D;
     m = NEG_INF;
     l = 0.0f;
@@ -185,6 +187,58 @@ __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, int64_t b
     }
 }
 
+// The end of a tile's part: outputs where it is the only one.
+template <int TYPE, int D, int NW>
+__device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const Plan &plan, const Tile &t, int64_t base,
+                                       int kvhead, int wave, int64_t tile, int part, int s0, int s1, f32x16 (&o)[D / 32],
+                                       float m, float l)
+{
+    constexpr bool F16 = is_f16(TYPE);
+    constexpr int NB = D / 32;
+    const int G = a.heads / c.kvh;
+    // the lane's number as if it were not known before: what is derived from it need
+    // not be kept in registers through the steps
+    int lane = (int)__lane_id();
+    asm volatile("" : "+v"(lane));
+    const int h = lane >> 5, row = wave * ROWS + (lane & 31);
+    const bool live = row < t.rows;
+    const int token = live ? t.token0 + (t.head0 + row) / G : 0, head = kvhead * G + (live ? (t.head0 + row) % G : 0);
+    // A value that is infinite or NaN reaches, as 0 times itself, also rows that do
+    // not see its key.  Only outputs can show that (weights are a row's own).
+    bool odd = false;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[b][i]) < __builtin_inff());
+    if (__any(odd && l < __builtin_inff())) redo<TYPE, D>(c, a, t, base, kvhead, s0, s1, token, head, live ? t.pos0 + token : -1, o, m, l);
+
+    l += __shfl_xor(l, 32);
+    if (t.parts == 1) {
+        if (!live) return;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // no key seen, or every score -inf
+        char *to = static_cast<char *>(a.out) + ((int64_t)(t.first + token) * a.out_stride + (int64_t)head * D + h * 4) * 2;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<u32x2 *>(to + (b * 32 + i * 2) * 2) =
+                    u32x2{pack2<F16>(o[b][i] * inv, o[b][i + 1] * inv), pack2<F16>(o[b][i + 2] * inv, o[b][i + 3] * inv)};
+        if (a.lse && h == 0)
+            a.lse[(int64_t)(t.first + token) * a.heads + head] = l == 0.0f ? NEG_INF : (m + log2_(l)) * LN2;
+        return;
+    }
+    // a part: maxima, sums and outputs as the lanes hold them
+    const int64_t slot = ((tile * c.kvh + kvhead) * plan.splits + part) * NW + wave;
+    float *to = static_cast<float *>(a.work) + slot * (ROWS * (D + 4)) + lane * 4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4 *>(to + (b * 4 + i) * 256) = f32x4{o[b][i * 4], o[b][i * 4 + 1], o[b][i * 4 + 2], o[b][i * 4 + 3]};
+    float *ml = static_cast<float *>(a.work) + slot * (ROWS * (D + 4)) + ROWS * D + lane * 2;
+    *reinterpret_cast<float2 *>(ml) = float2{m, l};
+}
+
 template <int TYPE, int D, int NW>
 __global__ void __launch_bounds__(NW * SAE_WAVE, D == 256 ? 1 : 2)
 k_prefill(KvDev c, AttnArgs a, Plan plan)
@@ -193,6 +247,9 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     constexpr int PB = SAE_KV_BLOCK * D * 2;  // bytes of a page in LDS
     constexpr int KEYS = keys_of(D), PAGES = KEYS / SAE_KV_BLOCK, KT = KEYS / 32;
     constexpr int NM = D / 16, NB = D / 32;
+    // LDS reads in flight while as many products are taken (an 8-bit cache's stage
+    // leaves fewer registers)
+    constexpr int BATCH = FP8 ? 2 : 4;
     typedef Stage<TYPE, D, NW> St;
     // arrays of their own: the compiler then sees that a read of one does not depend
     // on loads into another
@@ -217,9 +274,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     // this lane's row
     const int wrow = wave * ROWS, row = wrow + n;
     const bool live = row < t.rows;
-    const int token = live ? t.token0 + (t.head0 + row) / G : 0;
-    const int head = kvhead * G + (live ? (t.head0 + row) % G : 0);
-    const int pos = live ? t.pos0 + token : -1;                   // keys lo .. pos are seen
+    const int pos = live ? t.pos0 + t.token0 + (t.head0 + row) / G : -1;  // keys lo .. pos are seen
     const int lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
     // the wave's first and last position (rows are in order of position)
     const bool full_rows = wrow + ROWS <= t.rows;
@@ -232,6 +287,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     {
         // a negative scale is the query's sign, a scale of zero a query of zeros
         const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, keep = a.scale == 0.0f ? 0u : ~0u;
+        const int token = live ? t.token0 + (t.head0 + row) / G : 0, head = kvhead * G + (live ? (t.head0 + row) % G : 0);
         const char *qr = static_cast<const char *>(a.q) +
                          ((int64_t)(t.first + token) * a.q_stride + (int64_t)head * D + h * 8) * 2;
 #pragma unroll
@@ -551,40 +607,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         }
     }
 
-    // A value that is infinite or NaN reaches, as 0 times itself, also rows that do
-    // not see its key.  Only outputs can show that (weights are a row's own).
-    bool odd = false;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[b][i]) < __builtin_inff());
-    if (__any(odd && l < __builtin_inff())) redo<TYPE, D>(c, a, t, base, kvhead, s0, s1, token, head, lo, pos, o, m, l);
-
-    l += __shfl_xor(l, 32);
-    if (t.parts == 1) {
-        if (!live) return;
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // no key seen, or every score -inf
-        char *to = static_cast<char *>(a.out) + ((int64_t)(t.first + token) * a.out_stride + (int64_t)head * D + h * 4) * 2;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<u32x2 *>(to + (b * 32 + i * 2) * 2) =
-                    u32x2{pack2<F16>(o[b][i] * inv, o[b][i + 1] * inv), pack2<F16>(o[b][i + 2] * inv, o[b][i + 3] * inv)};
-        if (a.lse && h == 0)
-            a.lse[(int64_t)(t.first + token) * a.heads + head] = l == 0.0f ? NEG_INF : (m + log2_(l)) * LN2;
-        return;
-    }
-    // a part: maxima, sums and outputs as the lanes hold them
-    const int64_t slot = ((tile * c.kvh + kvhead) * plan.splits + part) * NW + wave;
-    float *to = static_cast<float *>(a.work) + slot * (ROWS * (D + 4)) + lane * 4;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<f32x4 *>(to + (b * 4 + i) * 256) = f32x4{o[b][i * 4], o[b][i * 4 + 1], o[b][i * 4 + 2], o[b][i * 4 + 3]};
-    float *ml = static_cast<float *>(a.work) + slot * (ROWS * (D + 4)) + ROWS * D + lane * 2;
-    *reinterpret_cast<float2 *>(ml) = float2{m, l};
+    finish<TYPE, D, NW>(c, a, plan, t, base, kvhead, wave, tile, part, s0, s1, o, m, l);
 }
 
 // Adds a tile's parts, in order: lanes hold what they held in k_prefill, a wave
@@ -604,19 +627,29 @@ __global__ void __launch_bounds__(SAE_WAVE) k_prefill_join(KvDev c, AttnArgs a, 
     if (!__any(live)) return;
     const float *from = static_cast<const float *>(a.work) + ((tile * c.kvh + kvhead) * plan.splits * NW + wave) * (ROWS * (D + 4));
     const int64_t stride = (int64_t)NW * (ROWS * (D + 4));
+    constexpr int UN = 4;  // parts in flight
     float m = NEG_INF, l = 0.0f;
     f32x4 o[4] = {};
-    for (int p = 0; p < t.parts; ++p, from += stride) {
-        const float2 ml = *reinterpret_cast<const float2 *>(from + ROWS * D + lane * 2);
-        f32x4 x[4];
+    for (int p = 0; p < t.parts; p += UN) {
+        float2 ml[UN];
+        f32x4 y[UN][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const f32x4 *>(from + (b * 4 + i) * 256 + lane * 4);
-        const float top = fmaxf(m, ml.x), mu = top == NEG_INF ? 0.0f : top;
-        const float f0 = exp2_(m - mu), f1 = exp2_(ml.x - mu);
-        l = l * f0 + ml.y * f1;
+        for (int k = 0; k < UN; ++k) {
+            const float *at = from + min(p + k, t.parts - 1) * stride;  // past the end: not added below
+            ml[k] = *reinterpret_cast<const float2 *>(at + ROWS * D + lane * 2);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = o[i] * f0 + x[i] * f1;
-        m = top;
+            for (int e = 0; e < 4; ++e) y[k][e] = *reinterpret_cast<const f32x4 *>(at + (b * 4 + e) * 256 + lane * 4);
+        }
+#pragma unroll
+        for (int k = 0; k < UN; ++k) {
+            if (p + k >= t.parts) break;  // uniform
+            const float top = fmaxf(m, ml[k].x), mu = top == NEG_INF ? 0.0f : top;
+            const float f0 = exp2_(m - mu), f1 = exp2_(ml[k].x - mu);
+            l = l * f0 + ml[k].y * f1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = o[e] * f0 + y[k][e] * f1;
+            m = top;
+        }
     }
     if (!live) return;
     const int token = t.token0 + (t.head0 + row) / G, head = kvhead * G + (t.head0 + row) % G;
@@ -632,20 +665,24 @@ __global__ void __launch_bounds__(SAE_WAVE) k_prefill_join(KvDev c, AttnArgs a, 
 
 constexpr int WAVES = 4;
 
-Plan plan_of(const KvDev &c, int n_tokens, int heads, int kvh)
+Plan plan_of(const KvDev &c, int n_tokens, int heads, int kvh, int dim, int window)
 {
     Plan p;
     const int G = heads / kvh;
     p.tiles = c.qs ? (int)((int64_t)n_tokens * G / (WAVES * ROWS)) + c.n_seq : c.n_seq * ((G + WAVES * ROWS - 1) / (WAVES * ROWS));
     const int64_t items = (int64_t)p.tiles * kvh;
-    p.splits = items >= GROUPS ? 1 : (int)(GROUPS / items);
+    // no tile has more parts than MIN_SPLIT goes into the keys that it can see
+    int64_t keys = (int64_t)c.max_blocks * SAE_KV_BLOCK;
+    if (window > 0) keys = std::min(keys, (int64_t)window + WAVES * ROWS + keys_of(dim));
+    const int64_t most = std::max(std::min((int64_t)groups_of(dim) / std::max(items, (int64_t)1), (keys + keys_of(dim)) / MIN_SPLIT), (int64_t)1);
+    p.splits = (int)most;
     return p;
 }
 
 template <int TYPE, int D>
 hipError_t launch(const KvDev &c, const AttnArgs &a, hipStream_t s)
 {
-    const Plan p = plan_of(c, c.n_tokens, a.heads, c.kvh);
+    const Plan p = plan_of(c, c.n_tokens, a.heads, c.kvh, D, a.window);
     hipLaunchKernelGGL((k_prefill<TYPE, D, WAVES>), dim3(p.tiles * c.kvh * p.splits), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
@@ -661,8 +698,8 @@ hipError_t launch_dim(const KvDev &c, const AttnArgs &a, int dim, hipStream_t s)
 
 }  // namespace
 
-// Enough for every call: there are parts only where all workgroups are at most GROUPS.
-size_t prefill_work_bytes(int dim) { return (size_t)GROUPS * WAVES * ROWS * (dim + 4) * sizeof(float); }
+// Enough for every call: there are parts only where all workgroups are at most groups_of(dim).
+size_t prefill_work_bytes(int dim) { return (size_t)groups_of(dim) * WAVES * ROWS * (dim + 4) * sizeof(float); }
 
 // Whether the call's tiles fit one launch.
 bool prefill_fits(const KvDev &c, int heads)
