@@ -87,4 +87,35 @@ __device__ __forceinline__ float max_groups(float x)
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// A value that all lanes hold, in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uniform(long long x)
+{
+    return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+
+// Exclusive scan over a workgroup of NW waves; total in every thread.  lds: NW
+// values that nothing else uses.
+template <int NW, typename T>
+__device__ __forceinline__ T scan(T v, T &total, T *lds)
+{
+    const int lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
+    T s = v;
+#pragma unroll
+    for (int o = 1; o < SAE_WAVE; o <<= 1) {
+        const T u = __shfl_up(s, o);
+        if (lane >= o) s += u;
+    }
+    if (lane == SAE_WAVE - 1) lds[wave] = s;
+    __syncthreads();
+    T before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        if (w < wave) before += lds[w];
+        total += lds[w];
+    }
+    return before + s - v;
+}
+
 }  // namespace attn

@@ -83,29 +83,6 @@ struct Start {
     long long seq_at;           // number of its first step
 };
 
-// Exclusive scan over the workgroup's threads; total in every thread.
-template <typename T>
-__device__ __forceinline__ T scan(T v, T &total, T *lds)
-{
-    const int lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
-    T s = v;
-#pragma unroll
-    for (int o = 1; o < SAE_WAVE; o <<= 1) {
-        const T u = __shfl_up(s, o);
-        if (lane >= o) s += u;
-    }
-    if (lane == SAE_WAVE - 1) lds[wave] = s;
-    __syncthreads();
-    T before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        if (w < wave) before += lds[w];
-        total += lds[w];
-    }
-    return before + s - v;
-}
-
 __device__ __forceinline__ Start find_start(const KvDev &c, int window, int x, int groups)
 {
     __shared__ long long tmp[NW];
@@ -123,11 +100,11 @@ __device__ __forceinline__ Start find_start(const KvDev &c, int window, int x, i
             sum = cost_of(len, window);
         }
         uint32_t t32;
-        at = scan((uint32_t)sum, t32, tmp32);
+        at = scan<NW>((uint32_t)sum, t32, tmp32);
         total = t32;
     } else {
         for (int r = r0; r < r1; ++r) sum += cost_of(kv::seq_len(c, r), window);
-        at = scan(sum, total, tmp);
+        at = scan<NW>(sum, total, tmp);
     }
     s.per = steps_per(total, groups);
     s.begin = x * s.per;

@@ -35,6 +35,7 @@ constexpr int keys_of(int dim) { return dim == 256 ? 32 : 64; }
 constexpr int MIN_SPLIT = 128;   // keys of a split at least
 // Workgroups wanted: two per compute unit, one of the larger heads.
 constexpr int groups_of(int dim) { return dim == 256 ? 256 : 512; }
+constexpr int SHORT = 512;       // keys of a table whose sequences are not split
 constexpr float SLACK = 8.0f;    // of the running maximum, in powers of two
 
 // Everything written to LDS before it, by stores or by to_lds(), is whole after it.
@@ -54,68 +55,140 @@ __device__ __forceinline__ void to_lds(const char *from, char *to)
 }
 
 struct Plan {
-    int tiles;   // row tiles of a head (an upper bound), `splits` workgroups each
-    int splits;
+    int tiles;   // row tiles of a head (an upper bound)
+    int groups;  // workgroups per key-value head that fill the GPU, over which long tiles'
+                 // keys are split; 0: none is
+    int most;    // parts of a tile at most (from the keys that the table holds)
 };
 
 // The rows of a workgroup and the keys they see.
 struct Tile {
     int seq, first;        // first row of the sequence in the call's arrays
-    int tokens;            // its new tokens
-    int64_t row0;          // first row of the tile: token0 * G + head0
-    int token0, head0;
-    int rows;              // rows of the tile that there are
-    int pos0;              // position of its first new token (may be negative)
+    int token0, head0;     // first row of the tile: token0 * G + head0
+    int rows;              // rows of the tile that there are; 0: no such tile
+    int pos0;              // position of the sequence's first new token (may be negative)
     int len;
     int step0, steps;      // steps of keys_of(dim) keys the tile sees: step0 .. step0 + steps - 1
-    int parts;             // workgroups they are divided over
-    bool none;
 };
 
-__device__ __forceinline__ Tile tile_of(const KvDev &c, const AttnArgs &a, int64_t tile, int rows, int splits, int keys)
+// Tile `sub` of sequence seq.
+__device__ __forceinline__ Tile tile_of(const KvDev &c, const AttnArgs &a, int seq, int64_t sub, int rows, int keys)
 {
-    Tile t;
-    const int G = a.heads / c.kvh;
-    int64_t sub;
-    if (!c.qs) {
-        const int of_seq = (G + rows - 1) / rows;
-        t.seq = (int)(tile / of_seq);
-        sub = tile % of_seq;
-    } else {
-        // f(r) = q_start[r] G / rows + r: at least the tiles before sequence r
-        int lo = 0, n = c.n_seq;
-        while (n > 1) {
-            const int step = (n + SAE_WAVE - 1) / SAE_WAVE, r = lo + (int)__lane_id() * step;
-            const bool below = r < lo + n && (int64_t)c.qs[r] * G / rows + r <= tile;
-            const uint64_t m = __ballot(below);
-            const int last = m ? 63 - __clzll((long long)m) : 0, end = lo + n;
-            lo += last * step;
-            n = min(step, end - lo);
-        }
-        t.seq = __builtin_amdgcn_readfirstlane(lo);
-        sub = tile - ((int64_t)c.qs[t.seq] * G / rows + t.seq);
-    }
-    kv::seq_rows(c, t.seq, t.first, t.tokens);
-    t.row0 = sub * rows;
-    t.none = sub < 0 || t.row0 >= (int64_t)t.tokens * G;
-    t.len = kv::seq_len(c, t.seq);
-    t.pos0 = t.len - t.tokens;
-    t.step0 = t.steps = 0;
-    t.parts = 1;
-    if (t.none) return t;
-    const int64_t end = min(t.row0 + rows, (int64_t)t.tokens * G);
-    t.rows = (int)(end - t.row0);
-    t.token0 = (int)(t.row0 / G);
-    t.head0 = (int)(t.row0 % G);
-    const int p0 = t.pos0 + t.token0, p1 = t.pos0 + t.token0 + (t.head0 + t.rows - 1) / G;  // first and last position
-    const int lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0;
+    int first, tokens;
+    kv::seq_rows(c, seq, first, tokens);
+    const int len = kv::seq_len(c, seq), G = a.heads / c.kvh;
+    Tile t = {seq, first, 0, 0, 0, len - tokens, len, 0, 0};
+    const int64_t row0 = sub * rows;
+    if (sub < 0 || row0 >= (int64_t)tokens * G) return t;
+    t.rows = (int)min((int64_t)rows, (int64_t)tokens * G - row0);
+    t.token0 = (int)(row0 / G);
+    t.head0 = (int)(row0 % G);
+    const int p0 = t.pos0 + t.token0, p1 = p0 + (t.head0 + t.rows - 1) / G;  // first and last position
     if (p1 >= 0) {
-        t.step0 = lo / keys;
+        t.step0 = (a.window > 0 ? max(0, p0 - a.window + 1) : 0) / keys;
         t.steps = p1 / keys + 1 - t.step0;
     }
-    t.parts = min(splits, max(1, t.steps / (MIN_SPLIT / keys)));
     return t;
 }
+
+// Without split tiles: tile number `tile` of the call, sequences' tiles counted from
+// q_start[r] G / rows + r on (at least what the sequences before have).
+__device__ __forceinline__ Tile find_tile(const KvDev &c, const AttnArgs &a, int64_t tile, int rows, int keys)
+{
+    const int G = a.heads / c.kvh;
+    if (!c.qs) {
+        const int of_seq = (G + rows - 1) / rows;
+        return tile_of(c, a, (int)(tile / of_seq), tile % of_seq, rows, keys);
+    }
+    int lo = 0, n = c.n_seq;
+    while (n > 1) {  // 64 probes a round trip
+        const int step = (n + SAE_WAVE - 1) / SAE_WAVE, r = lo + (int)__lane_id() * step;
+        const bool below = r < lo + n && (int64_t)c.qs[r] * G / rows + r <= tile;
+        const uint64_t m = __ballot(below);
+        const int last = m ? 63 - __clzll((long long)m) : 0, end = lo + n;
+        lo += last * step;
+        n = min(step, end - lo);
+    }
+    lo = uniform(lo);
+    return tile_of(c, a, lo, tile - ((int64_t)c.qs[lo] * G / rows + lo), rows, keys);
+}
+
+// With split tiles: every tile of a sequence in as many parts as its length calls for,
+// so that a part has about the average work of a workgroup.  Workgroup x of a head
+// takes part `part` of `parts` of tile `sub` of sequence `seq`.
+struct Part {
+    int seq, part, parts;  // seq < 0: none
+    int64_t sub;
+};
+constexpr int PER_THREAD = 4;  // sequences of a thread at most
+
+template <int NW>
+__device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, const Plan &plan, int x, int rows, int keys)
+{
+    __shared__ long long tmp[2][NW], found_rest;
+    __shared__ int found_seq, found_parts;
+    const int G = a.heads / c.kvh, chunk = (c.n_seq + NW * SAE_WAVE - 1) / (NW * SAE_WAVE);
+    // tiles of sequence r, and the mean of their steps, about
+    auto size = [&](int r, int &tiles, int &steps) {
+        int first, tokens;
+        kv::seq_rows(c, r, first, tokens);
+        const int len = kv::seq_len(c, r);
+        tiles = (int)(((int64_t)tokens * G + rows - 1) / rows);
+        steps = (a.window > 0 ? min(a.window, len) : max(len - tokens / 2, 0)) / keys + 1;
+    };
+    auto share_of = [&](long long total) {
+        return (int)max((total + plan.groups - 1) / plan.groups, (long long)(MIN_SPLIT / keys));
+    };
+    if (c.n_seq == 1) {  // uniform: no scans
+        int tiles, steps;
+        size(0, tiles, steps);
+        const int parts = min(max(steps / share_of((long long)tiles * steps), 1), plan.most);
+        return {x < (long long)tiles * parts ? 0 : -1, x % parts, parts, x / parts};
+    }
+    const int r0 = min((int)threadIdx.x * chunk, c.n_seq);
+    int tiles[PER_THREAD], steps[PER_THREAD];
+    long long work = 0;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+        tiles[i] = steps[i] = 0;
+        if (i < chunk && r0 + i < c.n_seq) {
+            size(r0 + i, tiles[i], steps[i]);
+            work += (long long)tiles[i] * steps[i];
+        }
+    }
+    long long total;
+    scan<NW>(work, total, tmp[0]);
+    const int share = share_of(total);
+    long long count = 0;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+        steps[i] = min(max(steps[i] / share, 1), plan.most);  // parts from here on
+        count += (long long)tiles[i] * steps[i];
+    }
+    long long before = scan<NW>(count, total, tmp[1]);
+    if (x >= before && x < before + count) {  // one thread
+#pragma unroll
+        for (int i = 0; i < PER_THREAD; ++i) {
+            const long long k = (long long)tiles[i] * steps[i];
+            if (x >= before && x < before + k) {
+                found_seq = r0 + i;
+                found_parts = steps[i];
+                found_rest = x - before;
+            }
+            before += k;
+        }
+    }
+    __syncthreads();
+    if (x >= total) return {-1, 0, 1, 0};
+    const int parts = uniform(found_parts), rest = uniform((int)found_rest);
+    return {uniform(found_seq), rest % parts, parts, rest / parts};
+}
+
+// A split tile as the workspace has it, by the workgroup of its first part.
+struct Split {
+    int token, head0, rows;  // token: row of the call's arrays of its first token
+    int parts;               // in workgroups x .. x + parts - 1; < 2: none
+};
 
 // A step's keys or values on their way from the cache to LDS: 16-byte pieces of
 // a thread, unit i of the wave's 1 KiB units.
@@ -187,10 +260,23 @@ __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, int64_t b
     }
 }
 
+// The workspace: descriptions of workgroups 0 .. groups + tiles - 1, then per
+// workgroup, head and wave a part's outputs, maxima and sums as the lanes hold them.
+__device__ __forceinline__ float *parts_of(const AttnArgs &a, const Plan &plan)
+{
+    return reinterpret_cast<float *>(static_cast<Split *>(a.work) + (plan.groups + plan.tiles));
+}
+__host__ __device__ constexpr int64_t part_floats(int dim) { return ROWS * (dim + 4); }
+template <int D, int NW>
+__device__ __forceinline__ int64_t part_at(const KvDev &c, int64_t x, int kvhead, int wave)
+{
+    return ((x * c.kvh + kvhead) * NW + wave) * part_floats(D);
+}
+
 // The end of a tile's part: outputs where it is the only one.
 template <int TYPE, int D, int NW>
 __device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const Plan &plan, const Tile &t, int64_t base,
-                                       int kvhead, int wave, int64_t tile, int part, int s0, int s1, f32x16 (&o)[D / 32],
+                                       int kvhead, int wave, int x, bool whole, int s0, int s1, f32x16 (&o)[D / 32],
                                        float m, float l)
 {
     constexpr bool F16 = is_f16(TYPE);
@@ -213,7 +299,7 @@ __device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const 
     if (__any(odd && l < __builtin_inff())) redo<TYPE, D>(c, a, t, base, kvhead, s0, s1, token, head, live ? t.pos0 + token : -1, o, m, l);
 
     l += __shfl_xor(l, 32);
-    if (t.parts == 1) {
+    if (whole) {
         if (!live) return;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // no key seen, or every score -inf
         char *to = static_cast<char *>(a.out) + ((int64_t)(t.first + token) * a.out_stride + (int64_t)head * D + h * 4) * 2;
@@ -228,18 +314,17 @@ __device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const 
         return;
     }
     // a part: maxima, sums and outputs as the lanes hold them
-    const int64_t slot = ((tile * c.kvh + kvhead) * plan.splits + part) * NW + wave;
-    float *to = static_cast<float *>(a.work) + slot * (ROWS * (D + 4)) + lane * 4;
+    float *to = parts_of(a, plan) + part_at<D, NW>(c, x, kvhead, wave);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<f32x4 *>(to + (b * 4 + i) * 256) = f32x4{o[b][i * 4], o[b][i * 4 + 1], o[b][i * 4 + 2], o[b][i * 4 + 3]};
-    float *ml = static_cast<float *>(a.work) + slot * (ROWS * (D + 4)) + ROWS * D + lane * 2;
-    *reinterpret_cast<float2 *>(ml) = float2{m, l};
+            *reinterpret_cast<f32x4 *>(to + (b * 4 + i) * 256 + lane * 4) =
+                f32x4{o[b][i * 4], o[b][i * 4 + 1], o[b][i * 4 + 2], o[b][i * 4 + 3]};
+    *reinterpret_cast<float2 *>(to + ROWS * D + lane * 2) = float2{m, l};
 }
 
-template <int TYPE, int D, int NW>
+template <int TYPE, int D, int NW, bool SPLIT>
 __global__ void __launch_bounds__(NW * SAE_WAVE, D == 256 ? 1 : 2)
 k_prefill(KvDev c, AttnArgs a, Plan plan)
 {
@@ -257,19 +342,30 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     char *const lds_k[2] = {k_even, k_odd}, *const lds_v[2] = {v_even, v_odd};
 
     // blocks go round-robin over the XCDs: the key-value head varies fastest, so
-    // that the tiles that read the same keys tend to share an L2; long tiles
-    // (late ones of a prompt) come first
-    const int per = c.kvh * plan.splits;
-    const int64_t tile = plan.tiles - 1 - (int64_t)(blockIdx.x / per);
-    const int part = blockIdx.x % per / c.kvh, kvhead = blockIdx.x % c.kvh;
-    const Tile t = tile_of(c, a, tile, NW * ROWS, plan.splits, keys_of(D));
-    if (t.none || part >= t.parts) return;
-    const int G = a.heads / c.kvh;
+    // that the tiles that read the same keys tend to share an L2
+    const int x = blockIdx.x / c.kvh, kvhead = blockIdx.x % c.kvh, G = a.heads / c.kvh;
+    Tile t;
+    int part = 0, nparts = 1;
+    if constexpr (SPLIT) {
+        const Part p = find_part<NW>(c, a, plan, x, NW * ROWS, KEYS);
+        if (p.seq >= 0) t = tile_of(c, a, p.seq, p.sub, NW * ROWS, KEYS);
+        if (kvhead == 0 && threadIdx.x == 0)
+            // (parts past the grid: only with a q_start that decreases)
+            static_cast<Split *>(a.work)[x] = p.seq >= 0 && p.part == 0 && x + p.parts <= plan.groups + plan.tiles
+                                                  ? Split{t.first + t.token0, t.head0, t.rows, p.parts}
+                                                  : Split{0, 0, 0, 0};
+        if (p.seq < 0) return;
+        part = p.part;
+        nparts = p.parts;
+    } else {  // long tiles (late ones of a prompt) come first
+        t = find_tile(c, a, plan.tiles - 1 - (int64_t)x, NW * ROWS, KEYS);
+    }
+    if (t.rows == 0) return;
     const int lane = (int)__lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / SAE_WAVE);
     const int n = lane & 31, h = lane >> 5;
     const int64_t base = kv::seq_base(c, t.seq);
-    const int s0 = t.step0 + (int)((int64_t)t.steps * part / t.parts);
-    const int s1 = t.step0 + (int)((int64_t)t.steps * (part + 1) / t.parts);
+    const int s0 = t.step0 + (int)((int64_t)t.steps * part / nparts);
+    const int s1 = t.step0 + (int)((int64_t)t.steps * (part + 1) / nparts);
 
     // this lane's row
     const int wrow = wave * ROWS, row = wrow + n;
@@ -607,7 +703,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         }
     }
 
-    finish<TYPE, D, NW>(c, a, plan, t, base, kvhead, wave, tile, part, s0, s1, o, m, l);
+    finish<TYPE, D, NW>(c, a, plan, t, base, kvhead, wave, x, nparts == 1, s0, s1, o, m, l);
 }
 
 // Adds a tile's parts, in order: lanes hold what they held in k_prefill, a wave
@@ -617,16 +713,13 @@ __global__ void __launch_bounds__(SAE_WAVE) k_prefill_join(KvDev c, AttnArgs a, 
 {
     constexpr bool F16 = is_f16(TYPE);
     const int wave = blockIdx.y % NW, b = blockIdx.y / NW;
-    const int64_t tile = blockIdx.x / c.kvh;
-    const int kvhead = blockIdx.x % c.kvh, G = a.heads / c.kvh;
-    const Tile t = tile_of(c, a, tile, NW * ROWS, plan.splits, keys_of(D));
-    if (t.none || t.parts == 1) return;
+    const int x = blockIdx.x / c.kvh, kvhead = blockIdx.x % c.kvh, G = a.heads / c.kvh;
+    const Split t = static_cast<const Split *>(a.work)[x];
+    if (t.parts < 2 || wave * ROWS >= t.rows) return;
     const int lane = (int)__lane_id(), n = lane & 31, h = lane >> 5;
     const int row = wave * ROWS + n;
-    const bool live = row < t.rows;
-    if (!__any(live)) return;
-    const float *from = static_cast<const float *>(a.work) + ((tile * c.kvh + kvhead) * plan.splits * NW + wave) * (ROWS * (D + 4));
-    const int64_t stride = (int64_t)NW * (ROWS * (D + 4));
+    const float *from = parts_of(a, plan) + part_at<D, NW>(c, x, kvhead, wave);
+    const int64_t stride = c.kvh * NW * part_floats(D);
     constexpr int UN = 4;  // parts in flight
     float m = NEG_INF, l = 0.0f;
     f32x4 o[4] = {};
@@ -651,42 +744,51 @@ __global__ void __launch_bounds__(SAE_WAVE) k_prefill_join(KvDev c, AttnArgs a, 
             m = top;
         }
     }
-    if (!live) return;
-    const int token = t.token0 + (t.head0 + row) / G, head = kvhead * G + (t.head0 + row) % G;
+    if (row >= t.rows) return;
+    const int64_t token = t.token + (t.head0 + row) / G, head = kvhead * G + (t.head0 + row) % G;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    char *to = static_cast<char *>(a.out) + ((int64_t)(t.first + token) * a.out_stride + (int64_t)head * D + b * 32 + h * 4) * 2;
+    char *to = static_cast<char *>(a.out) + (token * a.out_stride + head * D + b * 32 + h * 4) * 2;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         *reinterpret_cast<u32x2 *>(to + i * 16) =
             u32x2{pack2<F16>(o[i][0] * inv, o[i][1] * inv), pack2<F16>(o[i][2] * inv, o[i][3] * inv)};
-    if (a.lse && h == 0 && b == 0)
-        a.lse[(int64_t)(t.first + token) * a.heads + head] = l == 0.0f ? NEG_INF : (m + log2_(l)) * LN2;
+    if (a.lse && h == 0 && b == 0) a.lse[token * a.heads + head] = l == 0.0f ? NEG_INF : (m + log2_(l)) * LN2;
 }
 
 constexpr int WAVES = 4;
 
-Plan plan_of(const KvDev &c, int n_tokens, int heads, int kvh, int dim, int window)
+int64_t tiles_of(const KvDev &c, int heads)
 {
-    Plan p;
-    const int G = heads / kvh;
-    p.tiles = c.qs ? (int)((int64_t)n_tokens * G / (WAVES * ROWS)) + c.n_seq : c.n_seq * ((G + WAVES * ROWS - 1) / (WAVES * ROWS));
-    const int64_t items = (int64_t)p.tiles * kvh;
+    const int64_t G = heads / c.kvh, rows = WAVES * ROWS;
+    return c.qs ? c.n_tokens * G / rows + c.n_seq : c.n_seq * ((G + rows - 1) / rows);
+}
+
+Plan plan_of(const KvDev &c, int heads, int dim, int window)
+{
+    Plan p = {(int)tiles_of(c, heads), 0, 1};
     // no tile has more parts than MIN_SPLIT goes into the keys that it can see
     int64_t keys = (int64_t)c.max_blocks * SAE_KV_BLOCK;
     if (window > 0) keys = std::min(keys, (int64_t)window + WAVES * ROWS + keys_of(dim));
-    const int64_t most = std::max(std::min((int64_t)groups_of(dim) / std::max(items, (int64_t)1), (keys + keys_of(dim)) / MIN_SPLIT), (int64_t)1);
-    p.splits = (int)most;
+    p.most = (int)std::min((keys + keys_of(dim)) / MIN_SPLIT, (int64_t)groups_of(dim));
+    if ((int64_t)p.tiles * c.kvh <= groups_of(dim) && c.n_seq <= PER_THREAD * WAVES * SAE_WAVE && keys > SHORT)
+        p.groups = std::max(groups_of(dim) / c.kvh, 1);
     return p;
 }
 
 template <int TYPE, int D>
 hipError_t launch(const KvDev &c, const AttnArgs &a, hipStream_t s)
 {
-    const Plan p = plan_of(c, c.n_tokens, a.heads, c.kvh, D, a.window);
-    hipLaunchKernelGGL((k_prefill<TYPE, D, WAVES>), dim3(p.tiles * c.kvh * p.splits), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
+    const Plan p = plan_of(c, a.heads, D, a.window);
+    if (!p.groups) {
+        hipLaunchKernelGGL((k_prefill<TYPE, D, WAVES, false>), dim3(p.tiles * c.kvh), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
+        return hipGetLastError();
+    }
+    // parts: at most a share of the work each, rounded up for every tile
+    const unsigned grid = (unsigned)((p.groups + p.tiles) * c.kvh);
+    hipLaunchKernelGGL((k_prefill<TYPE, D, WAVES, true>), dim3(grid), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.splits == 1) return e;
-    hipLaunchKernelGGL((k_prefill_join<TYPE, D, WAVES>), dim3(p.tiles * c.kvh, WAVES * (D / 32)), dim3(SAE_WAVE), 0, s, c, a, p);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_prefill_join<TYPE, D, WAVES>), dim3(grid, WAVES * (D / 32)), dim3(SAE_WAVE), 0, s, c, a, p);
     return hipGetLastError();
 }
 
@@ -698,16 +800,15 @@ hipError_t launch_dim(const KvDev &c, const AttnArgs &a, int dim, hipStream_t s)
 
 }  // namespace
 
-// Enough for every call: there are parts only where all workgroups are at most groups_of(dim).
-size_t prefill_work_bytes(int dim) { return (size_t)groups_of(dim) * WAVES * ROWS * (dim + 4) * sizeof(float); }
+// Enough for every call: keys are split only where there are no more tiles than groups_of(dim) in all.
+size_t prefill_work_bytes(int kvh, int dim)
+{
+    const size_t groups = (size_t)std::max(groups_of(dim) / kvh, 1) * 2;
+    return groups * sizeof(Split) + groups * kvh * WAVES * part_floats(dim) * sizeof(float);
+}
 
 // Whether the call's tiles fit one launch.
-bool prefill_fits(const KvDev &c, int heads)
-{
-    const int64_t G = heads / c.kvh, rows = WAVES * ROWS;
-    const int64_t tiles = c.qs ? c.n_tokens * G / rows + c.n_seq : c.n_seq * ((G + rows - 1) / rows);
-    return tiles * c.kvh < (1ll << 23);
-}
+bool prefill_fits(const KvDev &c, int heads) { return tiles_of(c, heads) * c.kvh < (1ll << 23); }
 
 hipError_t launch_prefill(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s)
 {

@@ -110,5 +110,5 @@ struct AttnArgs {
 hipError_t launch_decode(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s);
 hipError_t launch_prefill(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s);
 size_t decode_work_bytes(int heads, int kvh, int dim);
-size_t prefill_work_bytes(int dim);
+size_t prefill_work_bytes(int kvh, int dim);
 bool prefill_fits(const KvDev &c, int heads);

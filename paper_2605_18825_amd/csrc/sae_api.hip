@@ -632,7 +632,7 @@ sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
 
 static size_t attn_work_bytes(int heads, int kvh, int dim)
 {
-    const size_t d = decode_work_bytes(heads, kvh, dim), p = prefill_work_bytes(dim);
+    const size_t d = decode_work_bytes(heads, kvh, dim), p = prefill_work_bytes(kvh, dim);
     return d > p ? d : p;
 }
 
