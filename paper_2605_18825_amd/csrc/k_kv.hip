@@ -56,21 +56,61 @@ struct Place {
     int dead0, dead1;
 };
 
+// The sequence of a tile and what is known of it, found by the whole workgroup: its
+// threads look at 256 sequences in one round trip.
+struct Seq {
+    int r, q0, q1, len, inst;  // r < 0: none (a q_start that decreases)
+};
+
+__device__ __forceinline__ Seq find_seq(const KvDev &c, int64_t tile)
+{
+    __shared__ Seq found;
+    __shared__ int below[THREADS / SAE_WAVE];
+    if (!c.qs) {
+        const int r = (int)tile;
+        return {r, r, r + 1, c.len[r], c.inst ? c.inst[r] : 0};
+    }
+    // tiles before sequence r: at least the pages that those touch
+    auto before = [&](int r, int q) { return (int64_t)(q >> 4) + 2ll * r; };
+    int lo = 0, n = c.n_seq;
+    while (n > THREADS) {  // the answer lies in [lo, lo + n)
+        const int step = (n + THREADS - 1) / THREADS, r = lo + (int)threadIdx.x * step;
+        const uint64_t m = __ballot(r < lo + n && before(r, c.qs[r]) <= tile);
+        if (__lane_id() == 0) below[threadIdx.x / SAE_WAVE] = __popcll((long long)m);
+        __syncthreads();
+        int count = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / SAE_WAVE; ++w) count += below[w];
+        __syncthreads();
+        const int end = lo + n;
+        lo += max(count - 1, 0) * step;
+        n = min(step, end - lo);
+    }
+    if (threadIdx.x == 0) found.r = -1;
+    __syncthreads();
+    const int r = lo + (int)threadIdx.x;
+    if (r < lo + n) {
+        const Seq s = {r, c.qs[r], c.qs[r + 1], c.len[r], c.inst ? c.inst[r] : 0};
+        if (before(r, s.q0) <= tile && (r + 1 == c.n_seq || tile < before(r + 1, s.q1))) found = s;
+    }
+    __syncthreads();
+    return {__builtin_amdgcn_readfirstlane(found.r), __builtin_amdgcn_readfirstlane(found.q0),
+            __builtin_amdgcn_readfirstlane(found.q1), __builtin_amdgcn_readfirstlane(found.len),
+            __builtin_amdgcn_readfirstlane(found.inst)};
+}
+
 // Tile -> sequence and page.
 __device__ __forceinline__ Place place_of(const KvDev &c, int64_t tile)
 {
-    Place p;
-    int r;
-    int64_t sub = 0;  // the tile's number among its sequence's
-    if (c.qs) {
-        r = kv::find_seq(c, tile, 4, 2);
-        sub = tile - ((int64_t)(c.qs[r] >> 4) + 2ll * r);
-    } else {
-        r = (int)tile;
-    }
-    int first, count;
-    kv::seq_rows(c, r, first, count);
-    const int len = kv::seq_len(c, r);
+    Place p = {};
+    const Seq s = find_seq(c, tile);
+    p.none = true;
+    if (s.r < 0) return p;
+    const int r = s.r;
+    // the tile's number among its sequence's
+    const int64_t sub = c.qs ? tile - ((int64_t)(s.q0 >> 4) + 2ll * r) : 0;
+    const int first = min(max(s.q0, 0), c.n_tokens), count = min(max(s.q1, first), c.n_tokens) - first;
+    const int len = kv::checked_len(c, s.len);
     const int start = len - count;  // position of the first new token; < 0: the first -start rows have no place
     const int pos0 = max(start, 0);
     p.none = sub < 0 || count == 0 || ((pos0 >> 4) + sub) * SAE_KV_BLOCK >= len;
@@ -79,7 +119,7 @@ __device__ __forceinline__ Place place_of(const KvDev &c, int64_t tile)
     p.t_hi = min(len - (page << 4), SAE_KV_BLOCK);
     p.row0 = first - start + (page << 4);
     p.block = -1;
-    if (!p.none) p.block = kv::pool_block(c, kv::seq_base(c, r), c.ids[(int64_t)r * c.max_blocks + page]);
+    if (!p.none) p.block = kv::pool_block(c, kv::inst_base(c, s.inst), c.ids[(int64_t)r * c.max_blocks + page]);
     p.dead0 = p.dead1 = first;
     if (sub == 0 && start < 0) p.dead1 = first + min(count, -start);
     return p;

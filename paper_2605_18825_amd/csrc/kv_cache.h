@@ -38,16 +38,18 @@ __device__ __forceinline__ int checked_len(const KvDev &c, int n)
 
 __device__ __forceinline__ int seq_len(const KvDev &c, int r) { return checked_len(c, c.len[r]); }
 
-// First pool block of sequence r's instance, or -1.
-__device__ __forceinline__ int64_t seq_base(const KvDev &c, int r)
+// First pool block of instance i, or -1.
+__device__ __forceinline__ int64_t inst_base(const KvDev &c, int i)
 {
-    const int i = c.inst ? c.inst[r] : 0;
     if (i < 0 || i >= c.n_inst) {
         report(c);
         return -1;
     }
     return (int64_t)i * c.bpi;
 }
+
+// First pool block of sequence r's instance, or -1.
+__device__ __forceinline__ int64_t seq_base(const KvDev &c, int r) { return inst_base(c, c.inst ? c.inst[r] : 0); }
 
 // Pool block for table entry `id` of a sequence with that base; -1 for none.
 __device__ __forceinline__ int64_t pool_block(const KvDev &c, int64_t base, int id)
@@ -68,26 +70,6 @@ __device__ __forceinline__ void seq_rows(const KvDev &c, int r, int &first, int 
     const int a = min(max(c.qs[r], 0), c.n_tokens), b = min(max(c.qs[r + 1], a), c.n_tokens);
     first = a;
     count = b - a;
-}
-
-// The sequence r with f(r) <= tile < f(r + 1), f(r) = (q_start[r] >> shift) +
-// per_seq * r, which does not decrease: 64 probes a step, one per lane (a batch
-// of up to 4,096 sequences takes two round trips).  All lanes take part.
-__device__ __forceinline__ int find_seq(const KvDev &c, int64_t tile, int shift, int per_seq)
-{
-    int lo = 0, n = c.n_seq;  // the answer lies in [lo, lo + n)
-    while (n > 1) {
-        const int step = (n + SAE_WAVE - 1) / SAE_WAVE;
-        const int r = lo + (int)__lane_id() * step;
-        const bool below = r < lo + n && (int64_t)(c.qs[r] >> shift) + (int64_t)per_seq * r <= tile;
-        const uint64_t m = __ballot(below);
-        // probes below `tile` are a prefix (lane 0's always counts)
-        const int last = m ? 63 - __clzll((long long)m) : 0;
-        const int end = lo + n;
-        lo += last * step;
-        n = min(step, end - lo);
-    }
-    return lo;
 }
 
 }  // namespace kv
