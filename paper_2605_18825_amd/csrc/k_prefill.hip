@@ -32,7 +32,7 @@ constexpr int ROWS = 32;   // rows of a wave
 // Keys of a step: 64, or 32 where a row's state and a step's scores would not fit
 // the registers together.
 constexpr int keys_of(int dim) { return dim == 256 ? 32 : 64; }
-constexpr int MIN_SPLIT = 128;   // keys of a split at least
+constexpr int MIN_SPLIT = 192;   // keys of a split at least
 // Workgroups wanted: two per compute unit, one of the larger heads.
 constexpr int groups_of(int dim) { return dim == 256 ? 256 : 512; }
 constexpr int SHORT = 512;       // keys of a table whose sequences are not split
@@ -71,18 +71,18 @@ struct Tile {
     int step0, steps;      // steps of keys_of(dim) keys the tile sees: step0 .. step0 + steps - 1
 };
 
-// Tile `sub` of sequence seq.
-__device__ __forceinline__ Tile tile_of(const KvDev &c, const AttnArgs &a, int seq, int64_t sub, int rows, int keys)
+// Tile `sub` of sequence seq.  (A call has fewer than 2^30 rows of a head: 32 bits.)
+__device__ __forceinline__ Tile tile_of(const KvDev &c, const AttnArgs &a, int seq, int sub, int rows, int keys)
 {
     int first, tokens;
     kv::seq_rows(c, seq, first, tokens);
     const int len = kv::seq_len(c, seq), G = a.heads / c.kvh;
     Tile t = {seq, first, 0, 0, 0, len - tokens, len, 0, 0};
-    const int64_t row0 = sub * rows;
-    if (sub < 0 || row0 >= (int64_t)tokens * G) return t;
-    t.rows = (int)min((int64_t)rows, (int64_t)tokens * G - row0);
-    t.token0 = (int)(row0 / G);
-    t.head0 = (int)(row0 % G);
+    const int row0 = sub * rows, end = tokens * G;
+    if (sub < 0 || row0 >= end) return t;
+    t.rows = min(rows, end - row0);
+    t.token0 = (int)((uint32_t)row0 / (uint32_t)G);
+    t.head0 = row0 - t.token0 * G;
     const int p0 = t.pos0 + t.token0, p1 = p0 + (t.head0 + t.rows - 1) / G;  // first and last position
     if (p1 >= 0) {
         t.step0 = (a.window > 0 ? max(0, p0 - a.window + 1) : 0) / keys;
@@ -93,24 +93,25 @@ __device__ __forceinline__ Tile tile_of(const KvDev &c, const AttnArgs &a, int s
 
 // Without split tiles: tile number `tile` of the call, sequences' tiles counted from
 // q_start[r] G / rows + r on (at least what the sequences before have).
-__device__ __forceinline__ Tile find_tile(const KvDev &c, const AttnArgs &a, int64_t tile, int rows, int keys)
+__device__ __forceinline__ Tile find_tile(const KvDev &c, const AttnArgs &a, int tile, int rows, int keys)
 {
     const int G = a.heads / c.kvh;
     if (!c.qs) {
         const int of_seq = (G + rows - 1) / rows;
-        return tile_of(c, a, (int)(tile / of_seq), tile % of_seq, rows, keys);
+        return tile_of(c, a, tile / of_seq, tile % of_seq, rows, keys);
     }
+    auto before = [&](int r) { return (int)((uint32_t)(min(max(c.qs[r], 0), c.n_tokens) * G) / (uint32_t)rows) + r; };
     int lo = 0, n = c.n_seq;
     while (n > 1) {  // 64 probes a round trip
         const int step = (n + SAE_WAVE - 1) / SAE_WAVE, r = lo + (int)__lane_id() * step;
-        const bool below = r < lo + n && (int64_t)c.qs[r] * G / rows + r <= tile;
+        const bool below = r < lo + n && before(r) <= tile;
         const uint64_t m = __ballot(below);
         const int last = m ? 63 - __clzll((long long)m) : 0, end = lo + n;
         lo += last * step;
         n = min(step, end - lo);
     }
     lo = uniform(lo);
-    return tile_of(c, a, lo, tile - ((int64_t)c.qs[lo] * G / rows + lo), rows, keys);
+    return tile_of(c, a, lo, tile - before(lo), rows, keys);
 }
 
 // With split tiles: every tile of a sequence in as many parts as its length calls for,
@@ -118,9 +119,9 @@ __device__ __forceinline__ Tile find_tile(const KvDev &c, const AttnArgs &a, int
 // takes part `part` of `parts` of tile `sub` of sequence `seq`.
 struct Part {
     int seq, part, parts;  // seq < 0: none
-    int64_t sub;
+    int sub;
 };
-constexpr int PER_THREAD = 4;  // sequences of a thread at most
+constexpr int PER_THREAD = 2;  // sequences of a thread at most: there are no more than tiles, of which there are at most 512
 
 template <int NW>
 __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, const Plan &plan, int x, int rows, int keys)
@@ -133,7 +134,7 @@ __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, con
         int first, tokens;
         kv::seq_rows(c, r, first, tokens);
         const int len = kv::seq_len(c, r);
-        tiles = (int)(((int64_t)tokens * G + rows - 1) / rows);
+        tiles = (int)((uint32_t)(tokens * G + rows - 1) / (uint32_t)rows);
         steps = (a.window > 0 ? min(a.window, len) : max(len - tokens / 2, 0)) / keys + 1;
     };
     auto share_of = [&](long long total) {
@@ -358,7 +359,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         part = p.part;
         nparts = p.parts;
     } else {  // long tiles (late ones of a prompt) come first
-        t = find_tile(c, a, plan.tiles - 1 - (int64_t)x, NW * ROWS, KEYS);
+        t = find_tile(c, a, plan.tiles - 1 - x, NW * ROWS, KEYS);
     }
     if (t.rows == 0) return;
     const int lane = (int)__lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / SAE_WAVE);
@@ -371,7 +372,9 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     const int wrow = wave * ROWS, row = wrow + n;
     const bool live = row < t.rows;
     const int pos = live ? t.pos0 + t.token0 + (t.head0 + row) / G : -1;  // keys lo .. pos are seen
-    const int lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+    // a row that sees nothing: a first key past all others
+    const int lo = pos < 0 ? 1 << 30 : a.window > 0 ? max(0, pos - a.window + 1) : 0;
+    const uint32_t span = pos < 0 ? 0u : (uint32_t)(pos - lo);
     // the wave's first and last position (rows are in order of position)
     const bool full_rows = wrow + ROWS <= t.rows;
     const int wp0 = wrow < t.rows ? t.pos0 + t.token0 + (t.head0 + wrow) / G : -1;
@@ -523,14 +526,22 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         const int t0 = step * KEYS;
         if (holes == 0 && full_rows && t0 + KEYS - 1 <= wp0 && t0 >= wlo1) return;  // uniform
         asm volatile("");  // a branch: the comparisons are not worth taking on every step
+        const uint32_t rel = (uint32_t)(t0 + h * 4 - lo);  // lo <= key <= pos: key - lo, without sign, is at most span
 #pragma unroll
         for (int u = 0; u < KT; ++u)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int p = u * 2 + i / 8;
-                const int key = t0 + p * SAE_KV_BLOCK + (i / 4 % 2) * 8 + h * 4 + i % 4;
-                if (key < lo || key > pos || (holes >> p & 1)) s[u][i] = NEG_INF;
-            }
+            for (int i = 0; i < 16; ++i)
+                if (rel + (uint32_t)(u * 32 + i / 4 * 8 + i % 4) > span) s[u][i] = NEG_INF;
+        if (holes) {
+            asm volatile("");
+#pragma unroll
+            for (int p = 0; p < PAGES; ++p)
+                if (holes >> p & 1) {
+                    asm volatile("");
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[p / 2][p % 2 * 8 + i] = NEG_INF;
+                }
+        }
     };
     // The maximum of a step's scores, in powers of two.
     auto maximum = [&](const f32x16 (&s)[KT]) {
@@ -563,8 +574,8 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
                 w[u * 2 + i / 8][i / 2 % 4] = pack2<F16>(x, y);
             }
     };
-    auto outputs = [&](const u32x4 (&w)[PAGES], int buf) {
-        const char *vp = lds_v[buf] + vfrag;
+    auto outputs = [&](const u32x4 (&w)[PAGES], const char *lds) {
+        const char *vp = lds + vfrag;
 #pragma unroll
         for (int p = 0; p < PAGES; ++p)
 #pragma unroll
@@ -687,20 +698,21 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
             ++step;
         };
         f32x16 t[KT];
-        while (step + 2 < s1) {
+        while (step + 1 < s1) {  // two steps a round, each on its own buffers
             body(s, t, 0);
+            if (step + 1 >= s1) break;
             body(t, s, 1);
         }
-        if (step + 1 < s1) {
-            body(s, t, 0);
-            clean_v(step, holes0, v_odd);
-            weights(t, w);
-            outputs(w, 1);
-        } else {
-            clean_v(step, holes0, v_even);
-            weights(s, w);
-            outputs(w, 0);
+        // the last step: its scores are in t after an odd number of steps
+        const bool odd = (step - s0) & 1;
+        if (odd) {
+#pragma unroll
+            for (int u = 0; u < KT; ++u) s[u] = t[u];
         }
+        char *const last = odd ? v_odd : v_even;
+        clean_v(step, holes0, last);
+        weights(s, w);
+        outputs(w, last);
     }
 
     finish<TYPE, D, NW>(c, a, plan, t, base, kvhead, wave, x, nparts == 1, s0, s1, o, m, l);
