@@ -279,34 +279,26 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
                 if constexpr (FP8) w[e] *= scale_of(f.ks[e / 4], e % 4);
             }
             if (!v0 || !v1 || t0 < lo || t0 + STEP > len) {  // uniform: some key of the step is not seen
-                const bool there = vpage ? v1 : v0;
-                const int tl = t0 + (g >> 1) * SAE_KV_BLOCK + (g & 1) * 4;
-                uint32_t keep = 0;
+                asm volatile("");  // a branch: not worth taking on every step
+                // lo <= key < len of a page that is there: key - lo, without sign, is below seen
+                const uint32_t seen = (vpage ? v1 : v0) ? (uint32_t)(len - lo) : 0u;
+                const uint32_t rel = (uint32_t)(t0 + (g >> 1) * SAE_KV_BLOCK + (g & 1) * 4 - lo);
+                // a value that is not seen may be NaN: it becomes 0, and its scale byte too
+                uint32_t keep[4] = {0, 0, 0, 0};  // of the values: two 16-bit ones a word, or four bytes (two words)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int t = tl + (e / 4) * 8 + e % 4;
-                    if (there && t >= lo && t < len) keep |= 1u << e;
-                    else w[e] = NEG_INF;
+                    const bool there = rel + (uint32_t)(e / 4 * 8 + e % 4) < seen;
+                    if (!there) w[e] = NEG_INF;
+                    if constexpr (FP8) keep[e / 4] |= there ? 0xFFu << (8 * (e % 4)) : 0u;
+                    else keep[e / 2] |= there ? 0xFFFFu << (16 * (e % 2)) : 0u;
                 }
-                // a value that is not seen may be NaN: it becomes 0
 #pragma unroll
                 for (int i = 0; i < F::NV; ++i)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if constexpr (FP8) {  // bytes: 8 keys of one dimension, then of another
-#pragma unroll
-                            for (int b = 0; b < 4; ++b)
-                                if (!(keep >> (4 * (k & 1) + b) & 1)) f.v[i][k] &= ~(0xFFu << (8 * b));
-                        } else {
-#pragma unroll
-                            for (int b = 0; b < 2; ++b)
-                                if (!(keep >> (2 * k + b) & 1)) f.v[i][k] &= ~(0xFFFFu << (16 * b));
-                        }
-                    }
+                    for (int k = 0; k < 4; ++k) f.v[i][k] &= keep[FP8 ? k & 1 : k];
                 if constexpr (FP8) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (!(keep >> e & 1)) f.vs[e / 4] &= ~(0xFFu << (8 * (e % 4)));  // its scale byte too
+                    f.vs[0] &= keep[0];
+                    f.vs[1] &= keep[1];
                 }
             }
             float top = w[0];
