@@ -380,3 +380,13 @@ def test_prefill_one_token_each():
             out = torch.full_like(q, 7.0)
             call(kv, seqs, q, out, 0.1, work)
             assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol)
+
+
+def test_prefill_many_sequences():
+    """More sequences than a split call takes, long and short ones; and a batch whose longest is split the most."""
+    rng = np.random.default_rng(43)
+    new = rng.integers(0, 5, 700)
+    new[-1] = 1
+    run(O.BF16, 4, 2, 64, new + rng.integers(0, 70, 700), new=new, seed=44, lse=False)
+    run(O.F16, 4, 2, 64, [700, 6000, 3, 90, 2500], new=[30, 70, 3, 1, 200], seed=45)
+    run(O.FP8, 16, 2, 128, [9000], new=[150], seed=46)
