@@ -721,10 +721,10 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
 // Adds a tile's parts, in order: lanes hold what they held in k_prefill, a wave
 // one 32-dimension block of 32 rows.
 template <int TYPE, int D, int NW>
-__global__ void __launch_bounds__(SAE_WAVE) k_prefill_join(KvDev c, AttnArgs a, Plan plan)
+__global__ void __launch_bounds__(NW * SAE_WAVE) k_prefill_join(KvDev c, AttnArgs a, Plan plan)
 {
     constexpr bool F16 = is_f16(TYPE);
-    const int wave = blockIdx.y % NW, b = blockIdx.y / NW;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / SAE_WAVE), b = blockIdx.y;
     const int x = blockIdx.x / c.kvh, kvhead = blockIdx.x % c.kvh, G = a.heads / c.kvh;
     const Split t = static_cast<const Split *>(a.work)[x];
     if (t.parts < 2 || wave * ROWS >= t.rows) return;
@@ -800,7 +800,7 @@ hipError_t launch(const KvDev &c, const AttnArgs &a, hipStream_t s)
     hipLaunchKernelGGL((k_prefill<TYPE, D, WAVES, true>), dim3(grid), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_prefill_join<TYPE, D, WAVES>), dim3(grid, WAVES * (D / 32)), dim3(SAE_WAVE), 0, s, c, a, p);
+    hipLaunchKernelGGL((k_prefill_join<TYPE, D, WAVES>), dim3(grid, D / 32), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
     return hipGetLastError();
 }
 
