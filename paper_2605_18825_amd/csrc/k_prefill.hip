@@ -605,6 +605,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         }
         barrier();
         scores(s, 0);
+        barrier();  // every wave has read the first keys: the next loads go over them
         mask(s, s0, holes0);
         follow(maximum(s));
         int step = s0;
