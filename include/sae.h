@@ -615,7 +615,9 @@ sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
  * with products exact, sums in fp32 (exp under the running maximum) and one rounding
  * to the output's type.  A row that sees no key, or whose every s_t is -inf, gets
  * zeros and lse = -inf.  What lies in a block past the sequence's last position is
- * never used (it may be NaN).
+ * never used (it may be NaN).  A value that is infinite or NaN reaches the rows that
+ * see it, as something not finite, and no other (in sae_attn_prefill on a slow path:
+ * a workgroup that meets one takes about 130 times as long).
  *  q, out   device, [n_tokens][n_heads][head_dim] of `dtype`: the cache's type, bf16
  *           for an FP8 cache; strides and alignment as in sae_kv_write; out may not
  *           overlap any input
@@ -629,7 +631,8 @@ sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
  * sae_attn_decode takes one new token per sequence (q_start must be NULL, n_tokens =
  * n_seq): long sequences are split over the GPU and their parts joined.
  * sae_attn_prefill takes any number (the new tokens' keys and values are already in the
- * cache: causal attention over the cached prefix and themselves).
+ * cache: causal attention over the cached prefix and themselves), as long as
+ * (n_tokens * n_heads / 128 + n_seq * n_kv_heads) < 2^23, about.
  * Results do not depend on how the work is split but for the order of fp32 sums, and
  * that order depends on the call's arguments and lengths alone.
  */

@@ -21,6 +21,13 @@
 //     for j >= 4 token 8 + 4 (g % 2) + j - 4: the 8 tokens of a value page's
 //     16-byte piece.
 //
+// Bound by memory: 256 sequences of 512..2,048 tokens (8 heads of 128, bf16; 1.35 GB,
+// 1.36 GB fetched) 239 us, 5.6 TB/s; 131,072 tokens of the 8-bit cache 54.5 us and 4.8
+// for the join; of the matrix units' time 24 products of 16 cycles go with the 16 KB of a
+// step, a twelfth of what a compute unit could feed from memory.  So weights go into
+// the second product as two 16-bit numbers: its error is then that of the output's
+// rounding alone.  Smallest calls are round trips: 7 us, and 3.5 for a join.
+//
 // Work is divided evenly whatever the lengths: all sequences' steps lie one
 // after the other, and workgroup x takes steps x per .. (x + 1) per - 1 of its
 // head, found from the lengths alone (a scan in every workgroup: the host knows
@@ -38,10 +45,18 @@ constexpr int NW = 4, THREADS = NW * SAE_WAVE;
 constexpr int STEP = 32;       // keys a wave takes at a time: two pages
 constexpr int COLS = 16;       // query heads of a tile
 constexpr int MIN_STEPS = NW;  // steps of a workgroup at least (where there are as many)
-constexpr int EXTRA = 8;       // steps that a sequence costs beside its own
-// Bytes of keys and values up to which a sequence is left to one workgroup per head.
+// Steps that a sequence costs beside its own (37 sequences of 1..36,000 tokens: 0: 46.6
+// us, 4: 39.5, 8: 35.4, 16: 36.7; 256 of 512..2,048: 243 us up to 12, 248 at 16).
+constexpr int EXTRA = 8;
+// Bytes of keys and values up to which a sequence is left to one workgroup per head
+// (from the table's width: a second launch and the scan cost more than one compute
+// unit takes for them).  Drawn batches of short sequences, geometric means of 12 calls,
+// three draws: never 17.4 / 16.2 / 20.0 us, up to 192 KB 13.3 / 13.3 / 15.2, up to 400
+// KB 13.3 / 12.7 / 15.5, up to 1,000 KB 13.4 / 12.7 / 15.2.
 constexpr int64_t SINGLE = 384 << 10;
-constexpr int GROUPS = 512;    // workgroups of a call, about: two per compute unit
+// Workgroups of a call, about: two per compute unit (768: 247 us for the batch above, 65
+// for the long one; 1,024: 250 and 65).
+constexpr int GROUPS = 512;
 // Two values rounded to the 16-bit type, and what the rounding left, rounded too.
 template <bool F16>
 __device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo)

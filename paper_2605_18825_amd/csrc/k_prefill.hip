@@ -6,8 +6,8 @@
 // of them, over 64 keys (4 pages) a step, with the scores transposed:
 //   S^T = K Q^T (64 keys x 32 rows), P = exp(S - m), O^T += V^T P^T
 // on v_mfma_f32_32x32x16.  Keys and values of a step are staged in LDS, in the
-// cache's own page layout, double-buffered, the next step's loads in flight in
-// registers; an 8-bit cache is widened to bf16 (times its scale) on the way, once
+// cache's own page layout, double-buffered: 16-bit pages go there directly from
+// memory, an 8-bit cache through registers, widened to bf16 (times its scale) once
 // for all waves.  Queries, scores, weights and outputs never leave registers:
 // lane (n = lane % 32, h = lane / 32) holds all of row n's state (the other half
 // of its keys and dimensions in lane n ^ 32), and the 16 scores a lane holds of 32
@@ -18,8 +18,17 @@
 // The running maximum is followed loosely: outputs are rescaled only when some
 // row's maximum grew by more than 2^8, so weights are at most 2^8 (sums are fp32).
 //
+// Bound by the matrix units and the power they may draw: 8,192 tokens behind 4,096
+// cached ones, 32 heads of 128 on 8: 1,010 us, 1.09 PFLOP/s (a library product of
+// 8,192^3 reaches 1.15 on the same card).  The products are under way 59 % of the
+// time; the clock is 1.8 GHz then (2.0 GHz and 48 % before the loads went straight to
+// LDS and a step's products shared their time with another's exponentials).  Products
+// alone with five vector operations and two exponentials each reach 1.48 PFLOP/s.
+//
 // Where tiles are few, each one's keys are split over several workgroups, whose
-// unnormalised outputs k_prefill_join adds in order.
+// unnormalised outputs k_prefill_join adds in order.  Small calls are round trips and
+// code: a launch fetches its code anew, and the kernel's size (40 KB, now 28) was 25 %
+// of their time.  61 new tokens behind 1,440, 16 heads on 2: 13.8 + 5.2 us.
 #include <algorithm>
 
 #include "attn_tile.h"
@@ -32,11 +41,16 @@ constexpr int ROWS = 32;   // rows of a wave
 // Keys of a step: 64, or 32 where a row's state and a step's scores would not fit
 // the registers together.
 constexpr int keys_of(int dim) { return dim == 256 ? 32 : 64; }
-constexpr int MIN_SPLIT = 192;   // keys of a split at least
+// Keys of a split at least (drawn calls, geometric means of four times 16: 128 37.6 /
+// 45.1 / 23.4 / 29.2 us, 192 36.3 / 46.2 / 23.7 / 29.4, 256 37.5 / 46.2 / 23.5 / 29.0, 384
+// 36.3 / 47.3 / 24.3 / 29.0).
+constexpr int MIN_SPLIT = 192;
 // Workgroups wanted: two per compute unit, one of the larger heads.
 constexpr int groups_of(int dim) { return dim == 256 ? 256 : 512; }
-constexpr int SHORT = 512;       // keys of a table whose sequences are not split
-constexpr float SLACK = 8.0f;    // of the running maximum, in powers of two
+// Keys of a table whose sequences are not split: no second launch (256: 49.3 / 60.0 / 29.8
+// / 36.4 us, 512: 48.8 / 59.4 / 29.7 / 35.4, 1,024: 49.9 / 65.8 / 31.1 / 35.0).
+constexpr int SHORT = 512;
+constexpr float SLACK = 8.0f;  // of the running maximum, in powers of two
 
 // Everything written to LDS before it, by stores or by to_lds(), is whole after it.
 __device__ __forceinline__ void barrier()
@@ -121,7 +135,7 @@ struct Part {
     int seq, part, parts;  // seq < 0: none
     int sub;
 };
-constexpr int PER_THREAD = 2;  // sequences of a thread at most: there are no more than tiles, of which there are at most 512
+constexpr int PER_THREAD = 2;  // sequences of a thread at most: no more than tiles, which are 512 at most
 
 template <int NW>
 __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, const Plan &plan, int x, int rows, int keys)
@@ -206,7 +220,8 @@ struct Stage {
 
 // The wave's rows over steps s0 .. s1 - 1 once more, one key at a time on the
 // vector units, each row adding the keys it sees and no other: the slow path
-// for values that are not finite.  Same state as the loop it replaces.
+// for values that are not finite (about 130 times as long as the loop it
+// replaces, with the same state after it).
 template <int TYPE, int D>
 __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, int64_t base, int kvhead, int s0, int s1, int token,
                      int head, int pos, f32x16 (&o)[D / 32], float &m, float &l)
@@ -768,6 +783,9 @@ __global__ void __launch_bounds__(NW * SAE_WAVE) k_prefill_join(KvDev c, AttnArg
     if (a.lse && h == 0 && b == 0) a.lse[token * a.heads + head] = l == 0.0f ? NEG_INF : (m + log2_(l)) * LN2;
 }
 
+// 128 rows a workgroup.  256 rows (8 waves, one workgroup per compute unit) read half as
+// much from L2: 990 us for the long prompt instead of 1,006, but 207 instead of 179
+// for sixteen ragged ones.
 constexpr int WAVES = 4;
 
 int64_t tiles_of(const KvDev &c, int heads)
