@@ -55,12 +55,14 @@ __device__ __forceinline__ float high(uint32_t x)
     else return __uint_as_float(x & 0xFFFF0000u);
 }
 
-// Four e4m3 values times a power of two, as bf16 (exact but for results under 2^-126).
-__device__ __forceinline__ u32x2 widen4(uint32_t x, float scale)
+// Two e4m3 values, bytes 0 and 1 or 2 and 3, times a power of two, as bf16 (exact but
+// for results under 2^-126).
+template <bool HIGH>
+__device__ __forceinline__ uint32_t widen2(uint32_t x, float scale)
 {
-    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true))};
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, HIGH));
 }
+__device__ __forceinline__ u32x2 widen4(uint32_t x, float scale) { return u32x2{widen2<false>(x, scale), widen2<true>(x, scale)}; }
 __device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi, float scale)
 {
     const u32x2 a = widen4(lo, scale), b = widen4(hi, scale);

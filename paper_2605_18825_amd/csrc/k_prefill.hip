@@ -19,7 +19,7 @@
 // row's maximum grew by more than 2^8, so weights are at most 2^8 (sums are fp32).
 //
 // Bound by the matrix units and the power they may draw: 8,192 tokens behind 4,096
-// cached ones, 32 heads of 128 on 8: 1,010 us, 1.09 PFLOP/s (a library product of
+// cached ones, 32 heads of 128 on 8: 1,005 us, 1.09 PFLOP/s (a library product of
 // 8,192^3 reaches 1.15 on the same card).  The products are under way 59 % of the
 // time; the clock is 1.8 GHz then (2.0 GHz and 48 % before the loads went straight to
 // LDS and a step's products shared their time with another's exponentials).  Products
@@ -396,20 +396,41 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     const int wp1 = wrow < t.rows ? t.pos0 + t.token0 + (t.head0 + min(wrow + ROWS, t.rows) - 1) / G : -1;
     const int wlo1 = a.window > 0 ? max(0, wp1 - a.window + 1) : 0;  // the last row's first key
 
+    // table entries of 16 steps: lane 4 j + p has page p of step ids_from + j, -1 for none
+    int ids = -1, ids_from = 0;
+    auto load_ids = [&](int step) __attribute__((always_inline)) {
+        ids_from = step;
+        const int page = step * PAGES + lane;
+        ids = -1;
+        if (page * SAE_KV_BLOCK < t.len && step + lane / PAGES < s1) ids = c.ids[(int64_t)t.seq * c.max_blocks + page];
+    };
+    auto check_ids = [&]() __attribute__((always_inline)) {
+        if (ids >= c.bpi) kv::report(c);
+        if (base < 0 || ids >= c.bpi) ids = -1;
+    };
+    auto fetch_ids = [&](int step) {
+        load_ids(step);
+        check_ids();
+    };
+    // The first table entries before the queries: the keys wait for them alone, and loads
+    // arrive in order (queries first: 5.5 us from here to the first keys, now 3.5; sixteen
+    // prompts of 600 tokens 98 us, now 93).
+    load_ids(s0);
+    __builtin_amdgcn_sched_barrier(0);
     const float sl = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * LOG2E;
     u32x4 q[NM];
     {
-        // a negative scale is the query's sign, a scale of zero a query of zeros
-        const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, keep = a.scale == 0.0f ? 0u : ~0u;
         const int token = live ? t.token0 + (t.head0 + row) / G : 0, head = kvhead * G + (live ? (t.head0 + row) % G : 0);
         const char *qr = static_cast<const char *>(a.q) +
                          ((int64_t)(t.first + token) * a.q_stride + (int64_t)head * D + h * 8) * 2;
 #pragma unroll
-        for (int i = 0; i < NM; ++i) {
-            q[i] = u32x4{0, 0, 0, 0};
-            if (live) q[i] = (*reinterpret_cast<const u32x4 *>(qr + i * 32) ^ flip) & keep;
+        for (int i = 0; i < NM; ++i) q[i] = u32x4{0, 0, 0, 0};
+        if (live) {
+#pragma unroll
+            for (int i = 0; i < NM; ++i) q[i] = *reinterpret_cast<const u32x4 *>(qr + i * 32);
         }
     }
+    __builtin_amdgcn_sched_barrier(0);
     f32x16 o[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -417,16 +438,6 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
     float m = NEG_INF, l = 0.0f;
 
-    // table entries of 16 steps: lane 4 j + p has page p of step ids_from + j, -1 for none
-    int ids = -1, ids_from = 0;
-    auto fetch_ids = [&](int step) {
-        ids_from = step;
-        const int page = step * PAGES + lane;
-        ids = -1;
-        if (page * SAE_KV_BLOCK < t.len && step + lane / PAGES < s1) ids = c.ids[(int64_t)t.seq * c.max_blocks + page];
-        if (ids >= c.bpi) kv::report(c);
-        if (base < 0 || ids >= c.bpi) ids = -1;
-    };
     // bit p: page p of the step has no block
     auto holes_of = [&](int step) {
         return (uint32_t)(__ballot(ids < 0) >> ((step - ids_from) * PAGES)) & ((1u << PAGES) - 1);
@@ -476,36 +487,45 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
 #pragma unroll
         for (int i = 0; i < St::UNITS; ++i) load_v1(step, st, to, i);
     };
-    auto store_k = [&](const St &st, char *lds) {
-        if constexpr (FP8) {
-#pragma unroll
-            for (int i = 0; i < St::UNITS; ++i) {  // 16 dimensions of token lane % 16
-                const int unit = wave * St::UNITS + i, p = unit / St::PER_PAGE, sub = unit % St::PER_PAGE;
-                char *to = lds + p * PB + (sub * 4 + (lane >> 4)) * 512 + (lane & 15) * 16;
-                const float ks = scale_of(st.s[i][0], 0);
-                *reinterpret_cast<u32x4 *>(to) = widen8(st.x[i][0], st.x[i][1], ks);
-                *reinterpret_cast<u32x4 *>(to + 256) = widen8(st.x[i][2], st.x[i][3], ks);
-            }
+    // Unit i of a stage widened to bf16 (times its tokens' scales) and stored.
+    auto store_k1 = [&](const St &st, char *lds, int i) __attribute__((always_inline)) {
+        if constexpr (FP8) {  // 16 dimensions of token lane % 16
+            const int unit = wave * St::UNITS + i, p = unit / St::PER_PAGE, sub = unit % St::PER_PAGE;
+            char *to = lds + p * PB + (sub * 4 + (lane >> 4)) * 512 + (lane & 15) * 16;
+            const float ks = scale_of(st.s[i][0], 0);
+            *reinterpret_cast<u32x4 *>(to) = widen8(st.x[i][0], st.x[i][1], ks);
+            *reinterpret_cast<u32x4 *>(to + 256) = widen8(st.x[i][2], st.x[i][3], ks);
         }
     };
-    auto store_v = [&](const St &st, char *lds) {
-        if constexpr (FP8) {
+    auto store_v1 = [&](const St &st, char *lds, int i) __attribute__((always_inline)) {
+        if constexpr (FP8) {  // 8 tokens of two dimensions
+            const int unit = wave * St::UNITS + i, p = unit / St::PER_PAGE, sub = unit % St::PER_PAGE;
+            u32x4 w[2];
 #pragma unroll
-            for (int i = 0; i < St::UNITS; ++i) {  // 8 tokens of two dimensions
-                const int unit = wave * St::UNITS + i, p = unit / St::PER_PAGE, sub = unit % St::PER_PAGE;
-#pragma unroll
-                for (int dd = 0; dd < 2; ++dd) {
-                    u32x4 w;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {  // tokens 2 j, 2 j + 1 of the piece
-                        const uint32_t x = st.x[i][dd * 2 + j / 2] >> (16 * (j & 1));
-                        w[j] = pack2<false>(__builtin_amdgcn_cvt_f32_fp8((int)x, 0) * scale_of(st.s[i][j / 2], 2 * (j & 1)),
-                                            __builtin_amdgcn_cvt_f32_fp8((int)x, 1) * scale_of(st.s[i][j / 2], 2 * (j & 1) + 1));
-                    }
-                    *reinterpret_cast<u32x4 *>(lds + p * PB + (sub * 2 + (lane >> 5)) * 1024 + dd * 512 + (flip & 31) * 16) = w;
-                }
+            for (int j = 0; j < 2; ++j) {
+                // tokens 4 j .. 4 j + 3: a token's two dimensions side by side share a scale and one
+                // conversion (each value by itself: 442 us for the long 8-bit prompts, so 423)
+                const uint32_t x = st.x[i][j], y = st.x[i][2 + j], sc = st.s[i][j];
+                const uint32_t a01 = __builtin_amdgcn_perm(y, x, 0x05010400u), a23 = __builtin_amdgcn_perm(y, x, 0x07030602u);
+                const uint32_t t0 = widen2<false>(a01, scale_of(sc, 0)), t1 = widen2<true>(a01, scale_of(sc, 1));
+                const uint32_t t2 = widen2<false>(a23, scale_of(sc, 2)), t3 = widen2<true>(a23, scale_of(sc, 3));
+                w[0][j * 2] = __builtin_amdgcn_perm(t1, t0, 0x05040100u);
+                w[1][j * 2] = __builtin_amdgcn_perm(t1, t0, 0x07060302u);
+                w[0][j * 2 + 1] = __builtin_amdgcn_perm(t3, t2, 0x05040100u);
+                w[1][j * 2 + 1] = __builtin_amdgcn_perm(t3, t2, 0x07060302u);
             }
+            char *to = lds + p * PB + (sub * 2 + (lane >> 5)) * 1024 + (flip & 31) * 16;
+            *reinterpret_cast<u32x4 *>(to) = w[0];
+            *reinterpret_cast<u32x4 *>(to + 512) = w[1];
         }
+    };
+    auto store_k = [&](const St &st, char *lds) {
+#pragma unroll
+        for (int i = 0; i < St::UNITS; ++i) store_k1(st, lds, i);
+    };
+    auto store_v = [&](const St &st, char *lds) {
+#pragma unroll
+        for (int i = 0; i < St::UNITS; ++i) store_v1(st, lds, i);
     };
     // Zeros in the values of keys past the sequence's end or without a block (they
     // may be NaN; their scores are masked).  The whole workgroup, or none of it.
@@ -605,7 +625,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         St sk, sv;
         f32x16 s[KT];
         u32x4 w[PAGES];
-        fetch_ids(s0);
+        check_ids();
         uint32_t holes0 = holes_of(s0), holes = 0;  // of the step whose values, and of the one whose scores come next
         {
             St k0;
@@ -614,6 +634,11 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
             load_v(s0, sv, v_even);
             load_k(next, sk, k_odd);
             holes = holes_of(next);
+            if (a.scale <= 0.0f) {  // a negative scale is the query's sign, a scale of zero a query of zeros
+                const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, keep = a.scale == 0.0f ? 0u : ~0u;
+#pragma unroll
+                for (int i = 0; i < NM; ++i) q[i] = (q[i] ^ flip) & keep;
+            }
             store_k(k0, k_even);
             store_v(sv, v_even);
             store_k(sk, k_odd);
@@ -702,12 +727,16 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
 #pragma unroll
                     for (int j = (i - LATE / 2) * 16 * KT / (N - LATE / 2); j < (i + 1 - LATE / 2) * 16 * KT / (N - LATE / 2); ++j)
                         if (i >= LATE / 2) top = fmaxf(top, s2[j / 16][j % 16]);
+                    // (beside the second half: behind them all, heads of 256 took 681 us where this takes 643)
+                    if (FP8 && i >= N / 2 && (i - N / 2) * 2 * St::UNITS % (N / 2) == 0) {
+                        const int u = (i - N / 2) * 2 * St::UNITS / (N / 2);
+                        if (u < St::UNITS) store_k1(sk, lds_k[buf], u);
+                        else store_v1(sv, lds_v[buf ^ 1], u - St::UNITS);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
             follow(max_halves(top) * sl);
-            store_k(sk, lds_k[buf]);
-            store_v(sv, lds_v[buf ^ 1]);
             holes0 = holes;
             holes = holes2;
             barrier();  // keys of step + 2 and values of step + 1 are whole, what they replaced was read before
