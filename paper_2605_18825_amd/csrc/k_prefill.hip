@@ -19,7 +19,7 @@
 // row's maximum grew by more than 2^8, so weights are at most 2^8 (sums are fp32).
 //
 // Bound by the matrix units and the power they may draw: 8,192 tokens behind 4,096
-// cached ones, 32 heads of 128 on 8: 1,005 us, 1.09 PFLOP/s (a library product of
+// cached ones, 32 heads of 128 on 8: 1,010 us, 1.09 PFLOP/s (a library product of
 // 8,192^3 reaches 1.15 on the same card).  The products are under way 59 % of the
 // time; the clock is 1.8 GHz then (2.0 GHz and 48 % before the loads went straight to
 // LDS and a step's products shared their time with another's exponentials).  Products
@@ -28,7 +28,7 @@
 // Where tiles are few, each one's keys are split over several workgroups, whose
 // unnormalised outputs k_prefill_join adds in order.  Small calls are round trips and
 // code: a launch fetches its code anew, and the kernel's size (40 KB, now 28) was 25 %
-// of their time.  61 new tokens behind 1,440, 16 heads on 2: 13.8 + 5.2 us.
+// of their time.  61 new tokens behind 1,440, 16 heads on 2: 13.6 + 5.2 us.
 #include <algorithm>
 
 #include "attn_tile.h"
