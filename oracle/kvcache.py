@@ -118,15 +118,20 @@ def attention(q, at, k, v, there, scale, window):
     return out, lse, mag, big
 
 
-def bounds(out, lse, mag, big, dim, dtype):
+def bounds(out, lse, mag, big, dim, dtype, weight=None, floor=0.0):
     """How far outputs of `dtype` and log-sum-exps may be off.
 
     Scores are sums of dim exact products in fp32: off by at most (dim + 4) 2^-24 of the sum of their magnitudes
     (the scale and the base of the exponential included), and the exponential by a few 2^-23: a weight's relative error
-    is rel.  Weights are rounded to the 16-bit type (its roundoff) for the product with the values, the normaliser is
-    not; sums of non-negative weights in fp32 add less than 2^-20.  Then one rounding of the result."""
+    is rel.  Weights are rounded for the product with the values, by at most `weight` relative (the 16-bit type's
+    roundoff where none is given; its square where a weight is taken as two such numbers); the normaliser is not.  Sums
+    of non-negative weights in fp32 add less than 2^-20.  Then one rounding of the result.
+
+    floor: what the weights' rounding may add to an output in all beside that, where the 16-bit type ends below them
+    (f16): the largest |value| times the number of keys times the type's half step, in units of a row's largest weight
+    (the normaliser is at least one such)."""
     u = ROUNDOFF[dtype]
     rel = (dim + 4) * 2.0 ** -24 * big + 2.0 ** -20
     tiny = 2.0 ** -25 if dtype == F16 else 2.0 ** -134  # half the smallest subnormal
-    return (u * np.abs(out) + (u + 2 * rel)[..., None] * mag * (1 + u) + tiny,
+    return (u * np.abs(out) + ((u if weight is None else weight) + 2 * rel)[..., None] * mag * (1 + u) + tiny + floor,
             rel + 2.0 ** -22 * np.abs(np.where(np.isfinite(lse), lse, 0)))

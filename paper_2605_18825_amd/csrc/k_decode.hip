@@ -25,7 +25,8 @@
 // 1.36 GB fetched) 239 us, 5.6 TB/s; 131,072 tokens of the 8-bit cache 54.5 us and 4.8
 // for the join; of the matrix units' time 24 products of 16 cycles go with the 16 KB of a
 // step, a twelfth of what a compute unit could feed from memory.  So weights go into
-// the second product as two 16-bit numbers: its error is then that of the output's
+// the second product as two 16-bit numbers, f16 ones 2^15 times as large (weights
+// down to 2^-40 of a head's largest count): its error is then that of the output's
 // rounding alone.  Smallest calls are round trips: 7 us, and 3.5 for a join.
 //
 // Work is divided evenly whatever the lengths: all sequences' steps lie one
@@ -57,6 +58,8 @@ constexpr int64_t SINGLE = 384 << 10;
 // Workgroups of a call, about: two per compute unit (768: 247 us for the batch above, 65
 // for the long one; 1,024: 250 and 65).
 constexpr int GROUPS = 512;
+constexpr float BIAS = 15.0f;  // of f16 weights' reference: weights up to 2^15
+
 // Two values rounded to the 16-bit type, and what the rounding left, rounded too.
 template <bool F16>
 __device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo)
@@ -232,7 +235,7 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
         f32x4 o[NO];
 #pragma unroll
         for (int i = 0; i < NO; ++i) o[i] = f32x4{0, 0, 0, 0};
-        float m = NEG_INF, l = 0.0f;
+        float m = NEG_INF, l = 0.0f;  // m: the reference of weights
 
         // table entries of the wave's next 32 steps: lane 2 j + u has page u of step j
         int ids = -1, ids_from = -1;
@@ -319,7 +322,7 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
             float top = w[0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) top = fmaxf(top, w[e]);
-            top = max_groups(top);
+            top = reference<F16>(max_groups(top), BIAS);
             if (__any(top > m)) {  // a head's maximum grew: what is summed so far shrinks
                 const float mn = fmaxf(m, top);
                 const float f0 = mn == NEG_INF ? 0.0f : exp2_(m - mn);
@@ -337,7 +340,8 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
                 if constexpr (FP8) w[e] *= scale_of(f.vs[e / 4], e % 4);
             }
             // the weights as two 16-bit numbers each: the product with the values
-            // costs twice the (idle) matrix units and keeps 16 bits or more of them
+            // costs twice the (idle) matrix units and keeps 16 bits or more of them (f16: 22, or
+            // what lies above 2^-39 of the largest)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 uint32_t h_, l_;

@@ -17,6 +17,9 @@
 //
 // The running maximum is followed loosely: outputs are rescaled only when some
 // row's maximum grew by more than 2^8, so weights are at most 2^8 (sums are fp32).
+// With f16 weights by more than 2^3.9, and weights are 2^12 times as large: they stay
+// under 2^15.9 (the type ends at 2^16) and lose bits only below 2^-26 of the maximum
+// that is followed, all below 2^-37.
 //
 // Bound by the matrix units and the power they may draw: 8,192 tokens behind 4,096
 // cached ones, 32 heads of 128 on 8: 1,010 us, 1.09 PFLOP/s (a library product of
@@ -50,7 +53,14 @@ constexpr int groups_of(int dim) { return dim == 256 ? 256 : 512; }
 // Keys of a table whose sequences are not split: no second launch (256: 49.3 / 60.0 / 29.8
 // / 36.4 us, 512: 48.8 / 59.4 / 29.7 / 35.4, 1,024: 49.9 / 65.8 / 31.1 / 35.0).
 constexpr int SHORT = 512;
-constexpr float SLACK = 8.0f;  // of the running maximum, in powers of two
+// Of the running maximum, in powers of two; and how far under it the reference of f16
+// weights is.  A smaller slack rescales more often, most at heads of 256 (16 ragged prompts
+// / the long one; weights of f16 not biased, SLACK 8: 172 / 1,125 us; 5.9 and 10: 179 / 1,143;
+// 3.9 and 12: 190 / 1,178; 2.9 and 13: 203 / 1,206; heads of 128: 402 us for the long
+// contexts, so 405).
+template <bool F16>
+constexpr float SLACK = F16 ? 3.9f : 8.0f;
+constexpr float BIAS = 12.0f;
 
 // Everything written to LDS before it, by stores or by to_lds(), is whole after it.
 __device__ __forceinline__ void barrier()
@@ -443,7 +453,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
-    float m = NEG_INF, l = 0.0f;
+    float m = NEG_INF, l = 0.0f;  // m: the reference of weights
 
     // bit p: page p of the step has no block
     auto holes_of = [&](int step) {
@@ -596,7 +606,8 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     };
     // Follows the maximum: outputs and sums shrink where it grew by more than SLACK.
     auto follow = [&](float top) {
-        if (!__any(top > m + SLACK)) return;
+        top = reference<F16>(top, BIAS);
+        if (!__any(top > m + SLACK<F16>)) return;
         const float mn = fmaxf(m, top);
         const float f = mn == NEG_INF ? 0.0f : exp2_(m - mn);
         m = mn;
