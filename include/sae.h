@@ -612,8 +612,13 @@ sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
  * of positions t <= p that have a block and, with window > 0, t > p - window:
  *   s_t = scale (q . k_t),  out = sum_t exp(s_t) v_t / sum_t exp(s_t),
  *   lse = ln sum_t exp(s_t)
- * with products exact, sums in fp32 (exp under the running maximum) and one rounding
- * to the output's type.  A row that sees no key, or whose every s_t is -inf, gets
+ * with products exact, sums in fp32 (exp under the running maximum) and the result
+ * rounded to the output's type.  Weights exp(s_t) are rounded for the product with v_t
+ * (lse and the divisor sum them as they are): in sae_attn_decode to two 16-bit numbers
+ * each, which leaves far less than the result's own rounding does; in sae_attn_prefill to
+ * one of the output's type, which adds at most 2^-8 (bf16) or 2^-11 (f16) of
+ * sum_t exp(s_t) |v_t| / sum_t exp(s_t), and to the mean error about a third.  f16 weights
+ * count down to 2^-40 (decode) and 2^-37 (prefill) of a row's largest.  A row that sees no key, or whose every s_t is -inf, gets
  * zeros and lse = -inf.  What lies in a block past the sequence's last position is
  * never used (it may be NaN).  A value that is infinite or NaN reaches the rows that
  * see it, as something not finite, and no other (in sae_attn_prefill on a slow path:
