@@ -527,7 +527,9 @@ sae_status sae_predict_sessions_noalloc(int32_t n, int32_t d, const uint16_t *h,
  *                of 16 bytes), or 0 for n_kv_heads * 16 * head_dim: a larger one
  *                lets the layers of a block lie together
  *  k_scale, v_scale  device uint8 (FP8 only): token t of block b, head h at
- *                b * scale_stride + 16 h + t; a byte s stands for 2^(s - 127);
+ *                b * scale_stride + 16 h + t; a byte s in 1 .. 254 stands for
+ *                2^(s - 127) (sae_kv_write makes no others; what 0 and 255 stand
+ *                for is not defined);
  *                16-byte aligned; scale_stride a multiple of 16, or 0 for
  *                16 * n_kv_heads
  *  status        device uint32 or NULL: SAE_ST_BAD_BLOCK is ORed into it where a
