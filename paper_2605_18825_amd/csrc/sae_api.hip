@@ -677,7 +677,10 @@ static sae_status attn(const char *name, bool decode, const sae_kv *kv, const sa
         return fail(nullptr, SAE_ERR_ARG, "too many rows for one call: n_tokens * n_heads / 128 + n_seq * n_kv_heads >= 2^23");
     if (!work || !aligned(work, 16) || work_bytes < attn_work_bytes(n_heads, kv->n_kv_heads, kv->head_dim))
         return fail(nullptr, SAE_ERR_ARG, "work must be 16-byte aligned and hold sae_attn_work_size bytes");
-    const AttnArgs a = {q, out, lse, q_stride, out_stride, scale, window, n_heads, work};
+    // No position reaches past the table: a longer window is that long (then no difference of
+    // a position, which may be as low as -n_tokens, and the window passes 32 bits).
+    const int32_t most = seqs->max_blocks * SAE_KV_BLOCK;
+    const AttnArgs a = {q, out, lse, q_stride, out_stride, scale, window < most ? window : most, n_heads, work};
     hipError_t e = (decode ? launch_decode : launch_prefill)(d, a, kv->type, kv->head_dim, s);
     return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, name);
 }

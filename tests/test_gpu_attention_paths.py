@@ -127,6 +127,15 @@ def test_prefill_values_that_are_not_finite_in_split_tiles(ty, heads, kvh, dim, 
     assert np.all(np.abs(lse - wl) <= tol_l)
 
 
+@pytest.mark.parametrize("ty", TYPES)
+def test_windows_past_every_position(ty):
+    """The largest window there is hides nothing, also where rows have negative positions."""
+    for window in (2 ** 31 - 1, 2 ** 31 - 20, 1 << 20):
+        Call(ty, 8, 2, 128, [5, 20, 0, 300], new=[40, 25, 3, 30], seed=57, window=window).check(False)
+        Call(ty, 8, 2, 128, [2000, 33], new=[40, 60], seed=58, window=window).check(False)
+        Call(ty, 8, 2, 128, [5, 0, 2000], seed=59, window=window).check(True)
+
+
 # ------------------------------------------------------------------- graph
 @pytest.mark.parametrize("ty", [O.BF16, O.FP8])
 def test_graph_replays_of_split_calls(ty):
