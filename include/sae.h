@@ -514,6 +514,9 @@ sae_status sae_predict_sessions_noalloc(int32_t n, int32_t d, const uint16_t *h,
  * Paged key-value cache: the keys and values that the pool's blocks stand for,
  * and the attention over them.
  *
+ * These calls take no context: they launch on the calling thread's current device,
+ * where all of a call's memory and its stream have to be.
+ *
  * A block holds the keys and values of SAE_KV_BLOCK = 16 consecutive tokens of
  * one sequence, for one model layer (a model has one sae_kv per layer, all with
  * the block ids of the one pool).  Per key-value head it has a page of keys, a

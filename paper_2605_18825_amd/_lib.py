@@ -71,6 +71,7 @@ class SaePool(ctypes.Structure):
 
 
 class SaeKv(ctypes.Structure):
+    device = None  # of its tensors, where they are known
     _fields_ = [
         ("type", ctypes.c_int32),
         ("n_instances", ctypes.c_int32),
@@ -88,6 +89,7 @@ class SaeKv(ctypes.Structure):
 
 
 class SaeSeqs(ctypes.Structure):
+    device = None
     _fields_ = [
         ("n_seq", ctypes.c_int32),
         ("max_blocks", ctypes.c_int32),

@@ -315,10 +315,28 @@ def _rows(t, heads, dim):
     return t.data_ptr(), s0 if n > 1 else heads * dim, ty, n
 
 
-def _raw_stream(t, stream):
-    """The stream's handle; by default the current one of t's device (a decode step is a few microseconds: the handle
-    is taken without making a stream object)."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
+def _same_device(what, tensors):
+    """The device of the tensors (those that are not None)."""
+    devices = {t.get_device() for t in tensors if t is not None}
+    if len(devices) > 1:
+        raise SaeError("%s are on different devices: %s" % (what, sorted(devices)))
+    return devices.pop() if devices else None
+
+
+def _raw_stream(kv, seqs, a, b, lse, work, stream):
+    """The stream's handle, the current one by default, for a call on these tensors.  Launches go to the current device:
+    everything has to be there.  (A decode step is a few microseconds: the handle is taken without making a stream, and
+    the checks are written out.)"""
+    here = torch._C._cuda_getDevice()
+    if (a.get_device() != here or b.get_device() != here or (work is not None and work.get_device() != here) or
+            (lse is not None and lse.get_device() != here) or kv.device not in (here, None) or
+            seqs.device not in (here, None)):
+        raise SaeError("a call's tensors must all be on the current device (%d)" % here)
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(here)
+    if stream.device_index != here:
+        raise SaeError("the stream must be on the current device (%d), it is on %d" % (here, stream.device_index))
+    return stream.cuda_stream
 
 
 def make_kv(type, n_instances, blocks_per_instance, n_kv_heads, head_dim, k, v, k_scale=None, v_scale=None, status=None,
@@ -353,6 +371,7 @@ def make_kv(type, n_instances, blocks_per_instance, n_kv_heads, head_dim, k, v, 
     if status is not None:
         kv.status = _ptr(status).value
     kv.tensors = (k, v, k_scale, v_scale, status)
+    kv.device = _same_device("the cache's tensors", kv.tensors)
     return kv
 
 
@@ -370,6 +389,7 @@ def make_seqs(block_ids, kv_len, q_start=None, inst=None):
         p = _ptr(t)
         setattr(s, name, p.value if p is not None else None)
     s.tensors = (block_ids, kv_len, q_start, inst)
+    s.device = _same_device("the sequences' tensors", s.tensors)
     return s
 
 
@@ -379,7 +399,8 @@ def _kv_move(fn, kv, seqs, k, v, stream):
     vp, vs, vt, vn = _rows(v, heads, dim)
     if kt != vt or n != vn:
         raise SaeError("k and v must have one type and one length")
-    st = fn(ctypes.byref(kv), ctypes.byref(seqs), n, kt, kp, ks, vp, vs, _raw_stream(k, stream))
+    st = fn(ctypes.byref(kv), ctypes.byref(seqs), n, kt, kp, ks, vp, vs,
+            _raw_stream(kv, seqs, k, v, None, None, stream))
     if st:
         _check(None, st)
 
@@ -420,7 +441,7 @@ def sae_attn_decode(kv, seqs, q, out, scale, work, window=0, lse=None, stream=No
     if n != seqs.n_seq:
         raise SaeError("q must have a row per sequence")
     st = _lib.load().sae_attn_decode(ctypes.byref(kv), ctypes.byref(seqs), heads, ty, qp, qs, op, os_, lp, scale,
-                                     window, wp, wn, _raw_stream(q, stream))
+                                     window, wp, wn, _raw_stream(kv, seqs, q, out, lse, work, stream))
     if st:
         _check(None, st)
 
@@ -429,7 +450,7 @@ def sae_attn_prefill(kv, seqs, q, out, scale, work, window=0, lse=None, stream=N
     """Causal attention of the new tokens over their sequences' caches: q, out [n_tokens][heads][head_dim]."""
     n, heads, ty, qp, qs, op, os_, lp, wp, wn = _attn_rows(kv, q, out, lse, work)
     st = _lib.load().sae_attn_prefill(ctypes.byref(kv), ctypes.byref(seqs), n, heads, ty, qp, qs, op, os_, lp, scale,
-                                      window, wp, wn, _raw_stream(q, stream))
+                                      window, wp, wn, _raw_stream(kv, seqs, q, out, lse, work, stream))
     if st:
         _check(None, st)
 

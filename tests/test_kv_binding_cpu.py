@@ -1,0 +1,129 @@
+"""The binding of the paged cache's calls: which tensors it takes.  No GPU: tensors that say they are on a device, and a
+library that only notes what it is called with."""
+import pytest
+import torch
+
+from paper_2605_18825_amd import _lib, api
+
+
+class On:
+    """A host tensor that passes for one on GPU `device`."""
+
+    def __init__(self, t, device=0):
+        self.t, self.device = t, device
+
+    is_cuda = True
+
+    def get_device(self):
+        return self.device
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+class Stream:
+    def __init__(self, device):
+        self.device_index, self.cuda_stream = device, 0x5000 + device
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The library's calls so far, (name, arguments); the current device is 0."""
+    seen = []
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: seen.append((name, a)) or 0
+    lib = Lib()
+    monkeypatch.setattr(_lib, "load", lambda: lib)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 0x100 + d, raising=False)
+    return seen
+
+
+def cache(dev=(0, 0, 0), ty=api.KV_BF16, dtype=torch.bfloat16, **kw):
+    k, v = (On(torch.zeros((4, 2, 16 * 64), dtype=dtype), d) for d in dev[:2])
+    if ty == api.KV_FP8:
+        kw = dict(dict(k_scale=On(torch.zeros((4, 2, 16), dtype=torch.uint8)),
+                       v_scale=On(torch.zeros((4, 2, 16), dtype=torch.uint8))), **kw)
+    return api.make_kv(ty, 1, 4, 2, 64, k, v, status=On(torch.zeros(1, dtype=torch.int32), dev[2]), **kw)
+
+
+def seqs(dev=0, len_dev=None):
+    return api.make_seqs(On(torch.zeros((3, 2), dtype=torch.int32), dev),
+                         On(torch.zeros(3, dtype=torch.int32), dev if len_dev is None else len_dev))
+
+
+def rows(heads, dev=0, n=3):
+    return On(torch.zeros((n, heads, 64), dtype=torch.bfloat16), dev)
+
+
+def run(kv, s, dev=(0, 0, 0, 0), stream=None):
+    """Every call once; a, b, lse, work on these devices."""
+    work, lse = On(torch.zeros(64, dtype=torch.uint8), dev[3]), On(torch.zeros((3, 4)), dev[2])
+    yield lambda: api.sae_kv_write(kv, s, rows(2, dev[0]), rows(2, dev[1]), stream=stream)
+    yield lambda: api.sae_kv_read(kv, s, rows(2, dev[0]), rows(2, dev[1]), stream=stream)
+    yield lambda: api.sae_attn_decode(kv, s, rows(4, dev[0]), rows(4, dev[1]), 0.1, work, lse=lse, stream=stream)
+    yield lambda: api.sae_attn_prefill(kv, s, rows(4, dev[0]), rows(4, dev[1]), 0.1, work, lse=lse, stream=stream)
+
+
+NAMES = ["sae_kv_write", "sae_kv_read", "sae_attn_decode", "sae_attn_prefill"]
+
+
+def test_the_current_devices_stream(calls):
+    for f in run(cache(), seqs()):
+        f()
+    assert [c[0] for c in calls] == NAMES and all(c[1][-1] == 0x100 for c in calls)
+    del calls[:]
+    for f in run(cache(), seqs(), stream=Stream(0)):
+        f()
+    assert [c[0] for c in calls] == NAMES and all(c[1][-1] == 0x5000 for c in calls)
+
+
+def test_another_device_is_refused(calls):
+    """Launches go to the current device: a call whose tensors are elsewhere would run on the wrong one."""
+    for f in run(cache((1, 1, 1)), seqs(1), (1, 1, 1, 1)):
+        with pytest.raises(api.SaeError, match="current device"):
+            f()
+    assert not calls
+
+
+@pytest.mark.parametrize("at", range(4))
+def test_one_tensor_elsewhere_is_refused(calls, at):
+    dev = [0, 0, 0, 0]
+    dev[at] = 1
+    for i, f in enumerate(run(cache(), seqs(), dev)):
+        if i < 2 and at >= 2:
+            continue  # no lse, no work
+        with pytest.raises(api.SaeError, match="current device"):
+            f()
+    assert not calls
+
+
+def test_cache_or_sequences_elsewhere_are_refused(calls):
+    for kv, s in ((cache((1, 1, 1)), seqs()), (cache(), seqs(1))):
+        for f in run(kv, s):
+            with pytest.raises(api.SaeError, match="current device"):
+                f()
+    assert not calls
+    for dev in ((0, 1, 0), (1, 0, 0), (0, 0, 1)):
+        with pytest.raises(api.SaeError, match="different devices"):
+            cache(dev)
+    with pytest.raises(api.SaeError, match="different devices"):
+        seqs(0, 1)
+
+
+def test_a_stream_elsewhere_is_refused(calls):
+    for f in run(cache(), seqs(), stream=Stream(1)):
+        with pytest.raises(api.SaeError, match="stream"):
+            f()
+    assert not calls
+
+
+def test_descriptions_made_by_hand(calls):
+    """A sae_kv and sae_seqs filled without make_kv and make_seqs name no device: the call's own tensors are checked."""
+    kv, s = _lib.SaeKv(), _lib.SaeSeqs()
+    kv.n_kv_heads, kv.head_dim, s.n_seq = 2, 64, 3
+    for f in run(kv, s):
+        f()
+    assert [c[0] for c in calls] == NAMES
