@@ -296,6 +296,9 @@ def sae_predict_sessions_noalloc(h_bf16, w, logit, pred=None, stream=None):
 KV_BLOCK = 16
 KV_BF16, KV_F16, KV_FP8 = 0, 1, 2
 _KV_DTYPE = {torch.bfloat16: KV_BF16, torch.float16: KV_F16}
+# what a cache's tensors may be, and its scales (bytes of an exponent)
+_KV_HELD = {KV_BF16: (torch.bfloat16,), KV_F16: (torch.float16,), KV_FP8: (torch.uint8, torch.float8_e4m3fn)}
+_KV_SCALES = (torch.uint8, torch.float8_e8m0fnu)
 
 
 def _rows(t, heads, dim):
@@ -342,32 +345,34 @@ def _raw_stream(kv, seqs, a, b, lse, work, stream):
 def make_kv(type, n_instances, blocks_per_instance, n_kv_heads, head_dim, k, v, k_scale=None, v_scale=None, status=None,
             block_stride=0, scale_stride=0):
     """One layer's paged cache over device tensors (see sae_kv in include/sae.h); it keeps them alive.  k and v are
-    bf16, f16, or 8-bit (uint8 or float8_e4m3fn) tensors of any shape that hold the cache from their first element on:
+    of the cache's type (8-bit: uint8 or float8_e4m3fn) and of any shape, and hold the cache from their first element on:
     contiguous, or with block_stride (values) a view whose first dimension is the block."""
     kv = SaeKv()
     kv.type, kv.n_instances, kv.blocks_per_instance = int(type), int(n_instances), int(blocks_per_instance)
     kv.n_kv_heads, kv.head_dim = int(n_kv_heads), int(head_dim)
     kv.block_stride, kv.scale_stride = int(block_stride), int(scale_stride)
-    size = 1 if type == KV_FP8 else 2
+    if kv.type not in _KV_HELD:
+        raise SaeError("unknown cache type")
     blocks = n_instances * blocks_per_instance
 
-    def place(name, t, size, stride, block):
+    def place(name, t, dtypes, stride, block):
         if t is None:
             return
         if not t.is_cuda:
             raise SaeError("expected a device tensor")
-        if t.element_size() != size:
-            raise SaeError("%s must have %d-byte values" % (name, size))
+        if t.dtype not in dtypes:
+            raise SaeError("%s must be %s for this type of cache" % (name, " or ".join(str(d)[6:] for d in dtypes)))
+        size = t.element_size()
         if stride == 0 and not t.is_contiguous():
             raise SaeError("expected a contiguous tensor")
         need = ((blocks - 1) * (stride or block) + block) * size
         if t.untyped_storage().nbytes() - t.storage_offset() * size < need:
             raise SaeError("%s holds fewer than %d blocks" % (name, blocks))
         setattr(kv, name, t.data_ptr())
-    place("k", k, size, kv.block_stride, n_kv_heads * KV_BLOCK * head_dim)
-    place("v", v, size, kv.block_stride, n_kv_heads * KV_BLOCK * head_dim)
-    place("k_scale", k_scale, 1, kv.scale_stride, n_kv_heads * KV_BLOCK)
-    place("v_scale", v_scale, 1, kv.scale_stride, n_kv_heads * KV_BLOCK)
+    place("k", k, _KV_HELD[kv.type], kv.block_stride, n_kv_heads * KV_BLOCK * head_dim)
+    place("v", v, _KV_HELD[kv.type], kv.block_stride, n_kv_heads * KV_BLOCK * head_dim)
+    place("k_scale", k_scale, _KV_SCALES, kv.scale_stride, n_kv_heads * KV_BLOCK)
+    place("v_scale", v_scale, _KV_SCALES, kv.scale_stride, n_kv_heads * KV_BLOCK)
     if status is not None:
         kv.status = _ptr(status).value
     kv.tensors = (k, v, k_scale, v_scale, status)

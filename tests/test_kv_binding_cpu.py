@@ -127,3 +127,29 @@ def test_descriptions_made_by_hand(calls):
     for f in run(kv, s):
         f()
     assert [c[0] for c in calls] == NAMES
+
+
+def test_types_of_the_cache(calls):
+    """Tensors of another type than the cache's would be read as something else."""
+    right = {api.KV_BF16: [torch.bfloat16], api.KV_F16: [torch.float16], api.KV_FP8: [torch.uint8, torch.float8_e4m3fn]}
+    every = [torch.bfloat16, torch.float16, torch.int16, torch.uint8, torch.int8, torch.float8_e4m3fn, torch.float8_e5m2,
+             torch.float32]
+    for ty, fine in right.items():
+        for dtype in every:
+            if dtype in fine:
+                cache(ty=ty, dtype=dtype)
+                continue
+            with pytest.raises(api.SaeError, match="k must be"):
+                cache(ty=ty, dtype=dtype)
+    k, v = On(torch.zeros(8192, dtype=torch.bfloat16)), On(torch.zeros(8192, dtype=torch.float16))
+    with pytest.raises(api.SaeError, match="v must be"):
+        api.make_kv(api.KV_BF16, 1, 4, 2, 64, k, v)
+    for dtype, fine in ((torch.uint8, True), (torch.float8_e8m0fnu, True), (torch.float8_e4m3fn, False), (torch.int8, False)):
+        sc = On(torch.zeros((4, 2, 16), dtype=torch.uint8).view(dtype))
+        if fine:
+            cache(ty=api.KV_FP8, dtype=torch.uint8, v_scale=sc)
+            continue
+        with pytest.raises(api.SaeError, match="v_scale must be"):
+            cache(ty=api.KV_FP8, dtype=torch.uint8, v_scale=sc)
+    with pytest.raises(api.SaeError, match="unknown cache type"):
+        cache(ty=3)
