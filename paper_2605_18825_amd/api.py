@@ -374,6 +374,8 @@ def make_kv(type, n_instances, blocks_per_instance, n_kv_heads, head_dim, k, v, 
     place("k_scale", k_scale, _KV_SCALES, kv.scale_stride, n_kv_heads * KV_BLOCK)
     place("v_scale", v_scale, _KV_SCALES, kv.scale_stride, n_kv_heads * KV_BLOCK)
     if status is not None:
+        if status.dtype not in (torch.int32, torch.uint32) or status.numel() < 1:
+            raise SaeError("status must hold a 32-bit integer")
         kv.status = _ptr(status).value
     kv.tensors = (k, v, k_scale, v_scale, status)
     kv.device = _same_device("the cache's tensors", kv.tensors)

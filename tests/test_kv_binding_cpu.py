@@ -153,3 +153,13 @@ def test_types_of_the_cache(calls):
             cache(ty=api.KV_FP8, dtype=torch.uint8, v_scale=sc)
     with pytest.raises(api.SaeError, match="unknown cache type"):
         cache(ty=3)
+
+
+def test_status_holds_a_word(calls):
+    """The status is a 32-bit word on the device: less is written past."""
+    k, v = (On(torch.zeros(8192, dtype=torch.bfloat16)) for _ in range(2))
+    for t in (torch.zeros(1, dtype=torch.uint8), torch.zeros(0, dtype=torch.int32), torch.zeros(1)):
+        with pytest.raises(api.SaeError, match="status"):
+            api.make_kv(api.KV_BF16, 1, 4, 2, 64, k, v, status=On(t))
+    for t in (torch.zeros(1, dtype=torch.int32), torch.zeros(3, dtype=torch.uint32)):
+        assert api.make_kv(api.KV_BF16, 1, 4, 2, 64, k, v, status=On(t)).status == t.data_ptr()
