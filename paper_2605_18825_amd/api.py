@@ -342,11 +342,37 @@ def _raw_stream(kv, seqs, a, b, lse, work, stream):
     return stream.cuda_stream
 
 
+def _check_blocks(name, t, blocks, stride, block):
+    """A view with `blocks` blocks along its first dimension (or first ones) has them `stride` values apart, each of them
+    `block` values in a row; a contiguous tensor of another shape is a buffer that holds them so."""
+    n = lead = 1
+    for lead, size in enumerate(t.shape[:-1], 1):
+        n *= size
+        if n >= blocks:
+            break
+    if t.is_contiguous() and (n != blocks or t.dim() < 2):
+        return
+    if t.dim() < 2 or n < blocks:
+        raise SaeError("%s must be contiguous, or have the blocks along its first dimension" % name)
+    apart = stride
+    for i in range(lead - 1, -1, -1):
+        if t.shape[i] > 1 and t.stride(i) != apart:
+            raise SaeError("%s has its blocks %d values apart, not %d" % (name, t.stride(i), apart))
+        apart *= t.shape[i]
+    row = 1
+    for size, step in zip(reversed(t.shape[lead:]), reversed(t.stride()[lead:])):
+        if size > 1 and step != row:
+            raise SaeError("a block of %s must be contiguous" % name)
+        row *= size
+    if row < block:
+        raise SaeError("a block of %s must hold %d values" % (name, block))
+
+
 def make_kv(type, n_instances, blocks_per_instance, n_kv_heads, head_dim, k, v, k_scale=None, v_scale=None, status=None,
             block_stride=0, scale_stride=0):
     """One layer's paged cache over device tensors (see sae_kv in include/sae.h); it keeps them alive.  k and v are
     of the cache's type (8-bit: uint8 or float8_e4m3fn) and of any shape, and hold the cache from their first element on:
-    contiguous, or with block_stride (values) a view whose first dimension is the block."""
+    contiguous, or with block_stride (values; scale_stride, bytes) a view whose first dimension is the block."""
     kv = SaeKv()
     kv.type, kv.n_instances, kv.blocks_per_instance = int(type), int(n_instances), int(blocks_per_instance)
     kv.n_kv_heads, kv.head_dim = int(n_kv_heads), int(head_dim)
@@ -365,6 +391,8 @@ def make_kv(type, n_instances, blocks_per_instance, n_kv_heads, head_dim, k, v, 
         size = t.element_size()
         if stride == 0 and not t.is_contiguous():
             raise SaeError("expected a contiguous tensor")
+        if stride:
+            _check_blocks(name, t, blocks, stride, block)
         need = ((blocks - 1) * (stride or block) + block) * size
         if t.untyped_storage().nbytes() - t.storage_offset() * size < need:
             raise SaeError("%s holds fewer than %d blocks" % (name, blocks))

@@ -163,3 +163,44 @@ def test_status_holds_a_word(calls):
             api.make_kv(api.KV_BF16, 1, 4, 2, 64, k, v, status=On(t))
     for t in (torch.zeros(1, dtype=torch.int32), torch.zeros(3, dtype=torch.uint32)):
         assert api.make_kv(api.KV_BF16, 1, 4, 2, 64, k, v, status=On(t)).status == t.data_ptr()
+
+
+def test_strides_of_the_cache(calls):
+    """With block_stride a view has to lie as it says."""
+    block, nb = 2 * 16 * 64, 4
+    whole = torch.zeros((nb, 3, block), dtype=torch.bfloat16)  # three layers of a block together
+    layer = [On(whole[:, i]) for i in range(3)]
+    kv = api.make_kv(api.KV_BF16, 1, nb, 2, 64, layer[1], layer[2], block_stride=3 * block)
+    assert kv.k == whole.data_ptr() + 2 * block and kv.v == whole.data_ptr() + 4 * block
+    for stride in (block, 2 * block, 6 * block):
+        with pytest.raises(api.SaeError, match="apart"):
+            api.make_kv(api.KV_BF16, 1, nb, 2, 64, layer[0], layer[0], block_stride=stride)
+    with pytest.raises(api.SaeError, match="contiguous"):
+        api.make_kv(api.KV_BF16, 1, nb, 2, 64, layer[0], layer[0])
+    # dimensions of a block in another order, or fewer than a block has
+    turned = torch.zeros((nb, 2, 64, 16), dtype=torch.bfloat16).transpose(2, 3)
+    with pytest.raises(api.SaeError, match="a block of k"):
+        api.make_kv(api.KV_BF16, 1, nb, 2, 64, On(turned), On(turned), block_stride=block)
+    less = torch.zeros((nb, 2 * block), dtype=torch.bfloat16)[:, :block - 64]
+    with pytest.raises(api.SaeError, match="a block of k"):
+        api.make_kv(api.KV_BF16, 1, nb, 2, 64, On(less), On(less), block_stride=2 * block)
+    # a flat buffer, padded blocks, a single block (whose stride is nothing's)
+    flat = On(whole.reshape(-1))
+    api.make_kv(api.KV_BF16, 1, nb, 2, 64, flat, flat, block_stride=2 * block)
+    padded = On(torch.zeros((nb, block + 64), dtype=torch.bfloat16))
+    api.make_kv(api.KV_BF16, 1, nb, 2, 64, padded, padded, block_stride=block + 64)
+    one = On(torch.zeros((1, block), dtype=torch.bfloat16))
+    api.make_kv(api.KV_BF16, 1, 1, 2, 64, one, one, block_stride=4 * block)
+    api.make_kv(api.KV_BF16, 1, 1, 2, 64, flat, flat, block_stride=4 * block)
+    # blocks over two dimensions (instance, block), more of them than are used
+    api.make_kv(api.KV_BF16, 2, 2, 2, 64, *[On(whole.view(2, 2, 3, block)[:, :, i]) for i in (0, 1)], block_stride=3 * block)
+    api.make_kv(api.KV_BF16, 1, 3, 2, 64, layer[0], layer[1], block_stride=3 * block)
+    with pytest.raises(api.SaeError, match="apart"):
+        every_second = On(torch.zeros((4, 2, 3, block), dtype=torch.bfloat16)[::2, :, 0])
+        api.make_kv(api.KV_BF16, 2, 2, 2, 64, every_second, every_second, block_stride=3 * block)
+    # scales likewise
+    pages = [On(torch.zeros((nb, block), dtype=torch.uint8)) for _ in range(2)]
+    sc = torch.zeros((nb, 2, 64), dtype=torch.uint8)
+    api.make_kv(api.KV_FP8, 1, nb, 2, 64, *pages, k_scale=On(sc[:, 0, :32]), v_scale=On(sc[:, 1, :32]), scale_stride=128)
+    with pytest.raises(api.SaeError, match="apart"):
+        api.make_kv(api.KV_FP8, 1, nb, 2, 64, *pages, k_scale=On(sc[:, 0, :32]), v_scale=On(sc[:, 1, :32]), scale_stride=64)
