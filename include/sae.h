@@ -626,8 +626,9 @@ sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
  * count down to 2^-40 (decode) and 2^-37 (prefill) of a row's largest.  A row that sees no key, or whose every s_t is -inf, gets
  * zeros and lse = -inf.  What lies in a block past the sequence's last position is
  * never used (it may be NaN).  A value that is infinite or NaN reaches the rows that
- * see it, as something not finite, and no other (in sae_attn_prefill on a slow path:
- * a workgroup that meets one takes about 130 times as long).
+ * see it, as something not finite, and no other (in sae_attn_prefill on a slow path where
+ * only some of the 32 query rows that are taken together see it: these take about 130
+ * times as long).
  *  q, out   device, [n_tokens][n_heads][head_dim] of `dtype`: the cache's type, bf16
  *           for an FP8 cache; strides and alignment as in sae_kv_write; out may not
  *           overlap any input

@@ -89,16 +89,16 @@ __device__ __forceinline__ float max_groups(float x)
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// The reference of weights for a maximum of `top` (both in powers of two): `bias` under it
-// where weights are f16, which loses bits under 2^-14 and everything under 2^-25, while
-// keys that far below the largest may make up an output together (one key of a high
-// score and a small value before many others).  Weights then use the type's range above
-// 1.  Sums, outputs and parts are under the same reference, so nothing is corrected
-// after.  Where fp32 does not hold top - bias to a few bits the reference is the maximum.
+// The reference of weights for a maximum of `top` (both in powers of two): `bias` under it.
+// Sums, outputs and parts are under the same reference, so nothing is corrected after.
+// f16 loses bits under 2^-14 and everything under 2^-25, and keys that far below the
+// largest may make up an output together (one key of a high score and a small value
+// before many others): f16 weights use the type's range above 1.  Where fp32 does not
+// hold top - bias to a few bits their reference is the maximum.
 template <bool F16>
 __device__ __forceinline__ float reference(float top, float bias)
 {
-    return F16 ? top - (fabsf(top) < 0x1p19f ? bias : 0.0f) : top;
+    return top - (!F16 || fabsf(top) < 0x1p19f ? bias : 0.0f);
 }
 
 // A value that all lanes hold, in a scalar register.

@@ -58,7 +58,8 @@ constexpr int64_t SINGLE = 384 << 10;
 // Workgroups of a call, about: two per compute unit (768: 247 us for the batch above, 65
 // for the long one; 1,024: 250 and 65).
 constexpr int GROUPS = 512;
-constexpr float BIAS = 15.0f;  // of f16 weights' reference: weights up to 2^15
+template <bool F16>
+constexpr float BIAS = F16 ? 15.0f : 0.0f;  // of the weights' reference: weights up to 2^BIAS
 
 // Two values rounded to the 16-bit type, and what the rounding left, rounded too.
 template <bool F16>
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(THREADS, D == 256 ? 1 : 2) k_decode(KvDev c, A
             float top = w[0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) top = fmaxf(top, w[e]);
-            top = reference<F16>(max_groups(top), BIAS);
+            top = reference<F16>(max_groups(top), BIAS<F16>);
             if (__any(top > m)) {  // a head's maximum grew: what is summed so far shrinks
                 const float mn = fmaxf(m, top);
                 const float f0 = mn == NEG_INF ? 0.0f : exp2_(m - mn);

@@ -20,10 +20,10 @@
 // error of the outputs is 1.3 to 1.4 times that of their own rounding.
 //
 // The running maximum is followed loosely: outputs are rescaled only when some
-// row's maximum grew by more than 2^8, so weights are at most 2^8 (sums are fp32).
-// With f16 weights by more than 2^3.9, and weights are 2^12 times as large: they stay
-// under 2^15.9 (the type ends at 2^16) and lose bits only below 2^-26 of the maximum
-// that is followed, all below 2^-37.
+// row's maximum grew by more than 2^8, and weights are then 2^-8 .. 1 times what they are
+// under the maximum itself (sums are fp32).  With f16 weights by more than 2^3.9, and
+// weights are 2^12 times as large: they stay under 2^15.9 (the type ends at 2^16) and
+// lose bits only below 2^-26 of the maximum that is followed, all below 2^-37.
 //
 // Bound by the matrix units and the power they may draw: 8,192 tokens behind 4,096
 // cached ones, 32 heads of 128 on 8: 1,010 us, 1.09 PFLOP/s (a library product of
@@ -57,14 +57,16 @@ constexpr int groups_of(int dim) { return dim == 256 ? 256 : 512; }
 // Keys of a table whose sequences are not split: no second launch (256: 49.3 / 60.0 / 29.8
 // / 36.4 us, 512: 48.8 / 59.4 / 29.7 / 35.4, 1,024: 49.9 / 65.8 / 31.1 / 35.0).
 constexpr int SHORT = 512;
-// Of the running maximum, in powers of two; and how far under it the reference of f16
-// weights is.  A smaller slack rescales more often, most at heads of 256 (16 ragged prompts
-// / the long one; weights of f16 not biased, SLACK 8: 172 / 1,125 us; 5.9 and 10: 179 / 1,143;
-// 3.9 and 12: 190 / 1,178; 2.9 and 13: 203 / 1,206; heads of 128: 402 us for the long
-// contexts, so 405).
+// Of the running maximum, in powers of two; and how far under it the reference of the
+// weights is.  bf16: above it, weights never pass 1 and outputs overflow no earlier than
+// their sums do.  f16: a smaller slack rescales more often, most at heads of 256 (16
+// ragged prompts / the long one; weights not biased, SLACK 8: 172 / 1,125 us; 5.9 and 10: 179
+// / 1,143; 3.9 and 12: 190 / 1,178; 2.9 and 13: 203 / 1,206; heads of 128: 402 us for the
+// long contexts, so 405).
 template <bool F16>
 constexpr float SLACK = F16 ? 3.9f : 8.0f;
-constexpr float BIAS = 12.0f;
+template <bool F16>
+constexpr float BIAS = F16 ? 12.0f : -8.0f;
 
 // Everything written to LDS before it, by stores or by to_lds(), is whole after it.
 __device__ __forceinline__ void barrier()
@@ -232,10 +234,42 @@ struct Stage {
     uint32_t s[UNITS][2];  // scale bytes of an 8-bit cache
 };
 
+// Whether any value of keys from .. to - 1 is not finite: the whole wave, a page at a time.
+// (An 8-bit value may also pass the range of bf16 with its scale.)
+template <int TYPE, int D>
+__device__ __forceinline__ bool any_odd(const KvDev &c, const Tile &t, int64_t base, int kvhead, int from, int to)
+{
+    constexpr bool FP8 = TYPE == SAE_KV_FP8;
+    constexpr int E = FP8 ? 1 : 2, PAGE = SAE_KV_BLOCK * D * E;
+    constexpr uint32_t INF = FP8 ? 0x7Fu : is_f16(TYPE) ? 0x7C00u : 0x7F80u;  // the bits that say it
+    const int lane = (int)__lane_id();
+    bool odd = false;
+#pragma unroll 1
+    for (int page = from / SAE_KV_BLOCK; page * SAE_KV_BLOCK < to; ++page) {
+        const int id = c.ids[(int64_t)t.seq * c.max_blocks + page], lo = from - page * SAE_KV_BLOCK, hi = to - page * SAE_KV_BLOCK;
+        if (base < 0 || id < 0 || id >= c.bpi) continue;  // uniform
+        const char *vp = c.v + (base + id) * c.block_bytes + (int64_t)kvhead * PAGE;
+#pragma unroll 1
+        for (int i = lane; i < PAGE / 16; i += SAE_WAVE) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(vp + i * 16);
+#pragma unroll
+            for (int j = 0; j < 16 / E; ++j) {
+                const int token = (i & 1) * 4 + (j >> 2 & 1) * 8 + (j & 3);
+                odd |= token >= lo && token < hi && (w[j * E / 4] >> (8 * E * (j % (4 / E))) & INF) == INF;
+            }
+        }
+        if constexpr (FP8) {
+            const int token = lane & 15;
+            odd |= token >= lo && token < hi && c.vs[(base + id) * c.scale_stride + kvhead * SAE_KV_BLOCK + token] >= 240;
+        }
+    }
+    return __any(odd);
+}
+
 // The wave's rows over steps s0 .. s1 - 1 once more, one key at a time on the
 // vector units, each row adding the keys it sees and no other: the slow path
-// for values that are not finite (about 130 times as long as the loop it
-// replaces, with the same state after it).
+// for values that are not finite and that not all of the rows see (about 130 times as
+// long as the loop it replaces, with the same state after it).
 template <int TYPE, int D>
 __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, int64_t base, int kvhead, int s0, int s1, int token,
                      int head, int pos, f32x16 (&o)[D / 32], float &m, float &l)
@@ -320,13 +354,23 @@ __device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const 
     const bool live = row < t.rows;
     const int token = live ? t.token0 + (t.head0 + row) / G : 0, head = kvhead * G + (live ? (t.head0 + row) % G : 0);
     // A value that is infinite or NaN reaches, as 0 times itself, also rows that do
-    // not see its key.  Only outputs can show that (weights are a row's own).
+    // not see its key.  Only outputs can show that (weights are a row's own), and it is wrong
+    // only where the key is not seen by all the wave's rows: keys before the last row's
+    // window or past the first row's position.  (A prefix that every row sees may hold
+    // anything: the call takes as long as ever.)
     bool odd = false;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[b][i]) < __builtin_inff());
-    if (__any(odd && l < __builtin_inff())) redo<TYPE, D>(c, a, t, base, kvhead, s0, s1, token, head, live ? t.pos0 + token : -1, o, m, l);
+    if (__any(live && odd && l < __builtin_inff())) {
+        const int k0 = s0 * keys_of(D), k1 = min(s1 * keys_of(D), t.len);
+        const int p0 = t.pos0 + t.token0 + (t.head0 + wave * ROWS) / G;
+        const int p1 = t.pos0 + t.token0 + (t.head0 + min(wave * ROWS + ROWS, t.rows) - 1) / G;
+        if (any_odd<TYPE, D>(c, t, base, kvhead, max(p0 + 1, k0), k1) ||
+            (a.window > 0 && any_odd<TYPE, D>(c, t, base, kvhead, k0, min(p1 - a.window + 1, k1))))
+            redo<TYPE, D>(c, a, t, base, kvhead, s0, s1, token, head, live ? t.pos0 + token : -1, o, m, l);
+    }
 
     l += __shfl_xor(l, 32);
     if (whole) {
@@ -610,7 +654,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     };
     // Follows the maximum: outputs and sums shrink where it grew by more than SLACK.
     auto follow = [&](float top) {
-        top = reference<F16>(top, BIAS);
+        top = reference<F16>(top, BIAS<F16>);
         if (!__any(top > m + SLACK<F16>)) return;
         const float mn = fmaxf(m, top);
         const float f = mn == NEG_INF ? 0.0f : exp2_(m - mn);

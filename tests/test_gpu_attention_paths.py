@@ -127,6 +127,82 @@ def test_prefill_values_that_are_not_finite_in_split_tiles(ty, heads, kvh, dim, 
     assert np.all(np.abs(lse - wl) <= tol_l)
 
 
+def nan_at(c, places):
+    """NaN in the values of head 1 at (sequence, position, dimension)."""
+    size = 1 if c.ty == O.FP8 else 2
+    page = O.unpack(c.cache.pages[1], c.dim, size, 1)
+    for r, t, d in places:
+        where = (c.ids[r, t // 16], 1, t % 16, d)
+        page[where] = {O.BF16: 0x7FC0, O.F16: 0x7E00, O.FP8: 0x7F}[c.ty]
+        c.cache.values[1][where] = np.nan
+    c.cache.pages[1] = O.pack(page, size, 1)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("heads,kvh,dim", [(4, 2, 64), (16, 2, 128), (4, 2, 256)])
+@pytest.mark.parametrize("window", [0, 900])
+@pytest.mark.parametrize("split", [True, False])
+def test_prefill_nan_in_a_prefix_that_every_row_sees(ty, heads, kvh, dim, window, split):
+    """NaN among the values of a cached prefix: every row gets it, at its dimensions alone, and the call takes no
+    longer than others do (a few times as long at most: it looks whether some row does not see the value)."""
+    if split:
+        lens, new, shared = [1500, 1400], [61, 30], 0
+    else:
+        lens, new, shared = np.full(260, 1100), np.ones(260, int) * 2, 500
+    c = Call(ty, heads, kvh, dim, lens, new=new, seed=60 + dim, window=window, shared=shared)
+    # every row of the last new tokens sees positions past len - window, and those before the new tokens
+    at = [(r, lens[r] - 200 + r % 7, (5 * r) % dim) for r in range(min(len(lens), 3))]
+    if shared:  # blocks that are in no other place
+        c.ids[c.ids >= shared - 3] -= 3
+        for r, t, _ in at:
+            c.ids[r, t // 16] = shared - 3 + r
+
+    def time():
+        kv = c.cache.device()
+        q = torch.as_tensor(c.qbits).view(DT[c.dtype]).cuda()
+        out = torch.empty_like(q)
+        seqs = api.make_seqs(dev32(c.ids), dev32(c.lens), q_start=dev32(c.starts))
+        work = torch.empty(api.sae_attn_work_size(kv, seqs, c.n, heads), dtype=torch.uint8, device="cuda")
+        best = 1e9
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(10):
+                api.sae_attn_prefill(kv, seqs, q, out, c.scale, work, window=window)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b) / 10)
+        return best
+    say("NaN in a prefix, type %d heads %d/%d dim %d window %d %s" % (ty, heads, kvh, dim, window, "split" if split else "whole"))
+    before = time()
+    nan_at(c, at)
+    after = time()
+    say("  %.1f us, with NaN %.1f us" % (before * 1e3, after * 1e3))
+    assert after < 5 * before
+    want, wl, mag, big = c.want()
+    got, lse = c.run(False)
+    fine = np.isfinite(want)
+    assert (~fine).any() and np.array_equal(fine, np.isfinite(got))
+    tol, tol_l = O.bounds(np.where(fine, want, 0), wl, np.where(fine, mag, 0), big, dim, c.dtype)
+    assert np.all(np.abs(got - np.where(fine, want, 0))[fine] <= tol[fine])
+    assert np.all(np.abs(lse - wl) <= tol_l)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_prefill_values_near_the_largest(dim):
+    """Values near bf16's largest, scores that grow by five powers of two every 64 keys: outputs do not overflow on the
+    way to a mean that does not, whatever reference the weights are taken under."""
+    def fill(c, ids, q):
+        q[:] = 1.0
+        c.values[1] = np.sign(c.values[1]) * 3e38
+        for r, n in enumerate(lens):
+            for t in range(n):  # one key of every 64 has all the weight, the later ones the more
+                x = np.log(2.0) * (5 * (t // 64) if t % 64 == 40 else -300.0)
+                c.values[0][ids[r, t // 16], :, t % 16] = x / dim ** 0.5
+    for lens, new in (([20, 90, 400], [3, 60, 40]), ([2000], [5])):
+        Call(O.BF16, 4, 2, dim, lens, new=new, seed=61, fill=fill).check(False)
+
+
 @pytest.mark.parametrize("ty", TYPES)
 def test_windows_past_every_position(ty):
     """The largest window there is hides nothing, also where rows have negative positions."""
