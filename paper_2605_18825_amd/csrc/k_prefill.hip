@@ -337,6 +337,15 @@ __device__ __forceinline__ int64_t part_at(const KvDev &c, int64_t x, int kvhead
     return ((x * c.kvh + kvhead) * NW + wave) * part_floats(D);
 }
 
+// An output, which is a mean of values: finite f16 ones have none past their largest, where
+// the weights' rounding could take it (to infinity).
+template <bool F16>
+__device__ __forceinline__ float mean(float x)
+{
+    if constexpr (F16) return fabsf(x) < __builtin_inff() ? __builtin_amdgcn_fmed3f(x, -65504.0f, 65504.0f) : x;
+    else return x;
+}
+
 // The end of a tile's part: outputs where it is the only one.
 template <int TYPE, int D, int NW>
 __device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const Plan &plan, const Tile &t, int64_t base,
@@ -384,7 +393,7 @@ __device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const 
                 // eight in a row (stores of 8 bytes: 3 % more for drawn calls, 5 % for 16 prompts of 600).
                 uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = pack2<F16>(o[b][i + 2 * e] * inv, o[b][i + 2 * e + 1] * inv);
+                for (int e = 0; e < 4; ++e) w[e] = pack2<F16>(mean<F16>(o[b][i + 2 * e] * inv), mean<F16>(o[b][i + 2 * e + 1] * inv));
                 const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
                 const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
                 if (live) *reinterpret_cast<u32x4 *>(to + (b * 32 + i * 2) * 2) = u32x4{x[0], y[0], x[1], y[1]};
@@ -874,7 +883,8 @@ __global__ void __launch_bounds__(NW * SAE_WAVE) k_prefill_join(KvDev c, AttnArg
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         *reinterpret_cast<u32x2 *>(to + i * 16) =
-            u32x2{pack2<F16>(o[i][0] * inv, o[i][1] * inv), pack2<F16>(o[i][2] * inv, o[i][3] * inv)};
+            u32x2{pack2<F16>(mean<F16>(o[i][0] * inv), mean<F16>(o[i][1] * inv)),
+                  pack2<F16>(mean<F16>(o[i][2] * inv), mean<F16>(o[i][3] * inv))};
     if (a.lse && h == 0 && b == 0) a.lse[token * a.heads + head] = l == 0.0f ? NEG_INF : (m + log2_(l)) * LN2;
 }
 

@@ -81,3 +81,23 @@ def test_scores_of_any_size(ty, size):
     for dim in (64, 128):
         Call(ty, 4, 2, dim, [1, 40, 300, 2100], seed=8, fill=fill).check(True)
         Call(ty, 4, 2, dim, [1, 40, 300, 2100], new=[1, 40, 90, 6], seed=9, fill=fill).check(False)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_means_of_f16s_largest_value(dim):
+    """Values of f16's largest, as clamped ones are: no mean of them is larger, whatever the weights' rounding.  Each
+    sequence has one key of all the weight, and a later one with a little more: a weight that f16 does not hold."""
+    rng = np.random.default_rng(10)
+    lens = np.where(np.arange(150) % 3 == 0, 700, 130) + np.arange(150) % 5
+
+    def fill(c, ids, q):
+        q[:] = 1.0
+        c.values[1] = np.where(c.values[1] < -1.5, -65504.0, 65504.0)
+        c.values[1][..., ::3] = 65504.0
+        c.values[0][:] = -300.0 / dim ** 0.5
+        for r in range(len(ids)):
+            for t, bits in ((7, 0.0), (101, 3.8 * rng.random())):
+                c.values[0][ids[r, t // 16], :, t % 16] = np.log(2.0) * bits / dim ** 0.5
+    Call(O.F16, 4, 2, dim, lens, new=np.full(150, 2), seed=11, fill=fill).check(False)
+    Call(O.F16, 4, 2, dim, lens[:9], new=np.full(9, 20), seed=12, fill=fill).check(False)
+    Call(O.F16, 4, 2, dim, lens, seed=13, fill=fill).check(True)
