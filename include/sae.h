@@ -628,7 +628,7 @@ sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
  * never used (it may be NaN).  A value that is infinite or NaN reaches the rows that
  * see it, as something not finite, and no other (in sae_attn_prefill on a slow path where
  * only some of the 32 query rows that are taken together see it: these take about 130
- * times as long).
+ * times as long; so do rows whose largest score is past 10^7 either way).
  *  q, out   device, [n_tokens][n_heads][head_dim] of `dtype`: the cache's type, bf16
  *           for an FP8 cache; strides and alignment as in sae_kv_write; out may not
  *           overlap any input

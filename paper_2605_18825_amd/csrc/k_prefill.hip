@@ -268,8 +268,8 @@ __device__ __forceinline__ bool any_odd(const KvDev &c, const Tile &t, int64_t b
 
 // The wave's rows over steps s0 .. s1 - 1 once more, one key at a time on the
 // vector units, each row adding the keys it sees and no other: the slow path
-// for values that are not finite and that not all of the rows see (about 130 times as
-// long as the loop it replaces, with the same state after it).
+// for values that are not finite and that not all of the rows see, and for scores past
+// 2^24 (about 130 times as long as the loop it replaces, with the same state after it).
 template <int TYPE, int D>
 __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, int64_t base, int kvhead, int s0, int s1, int token,
                      int head, int pos, f32x16 (&o)[D / 32], float &m, float &l)
@@ -372,11 +372,15 @@ __device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const 
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[b][i]) < __builtin_inff());
-    if (__any(live && odd && l < __builtin_inff())) {
+    // A weight's exponent is one fused product and difference, under a maximum that was
+    // rounded: where fp32 holds scores to whole numbers or less, the rounding would be an
+    // exponent that may be anything.  Such rows take the slow path as well.
+    const bool huge = fabsf(m) >= 0x1p24f && fabsf(m) < __builtin_inff();
+    if (__any(live && (huge || (odd && l < __builtin_inff())))) {
         const int k0 = s0 * keys_of(D), k1 = min(s1 * keys_of(D), t.len);
         const int p0 = t.pos0 + t.token0 + (t.head0 + wave * ROWS) / G;
         const int p1 = t.pos0 + t.token0 + (t.head0 + min(wave * ROWS + ROWS, t.rows) - 1) / G;
-        if (any_odd<TYPE, D>(c, t, base, kvhead, max(p0 + 1, k0), k1) ||
+        if (__any(live && huge) || any_odd<TYPE, D>(c, t, base, kvhead, max(p0 + 1, k0), k1) ||
             (a.window > 0 && any_odd<TYPE, D>(c, t, base, kvhead, k0, min(p1 - a.window + 1, k1))))
             redo<TYPE, D>(c, a, t, base, kvhead, s0, s1, token, head, live ? t.pos0 + token : -1, o, m, l);
     }

@@ -101,3 +101,19 @@ def test_means_of_f16s_largest_value(dim):
     Call(O.F16, 4, 2, dim, lens, new=np.full(150, 2), seed=11, fill=fill).check(False)
     Call(O.F16, 4, 2, dim, lens[:9], new=np.full(9, 20), seed=12, fill=fill).check(False)
     Call(O.F16, 4, 2, dim, lens, seed=13, fill=fill).check(True)
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("size", [2e8, 1e11, 1e15, 1e25])
+def test_scores_past_fp32s_whole_numbers(ty, size):
+    """Scores so large that fp32 holds them to hundreds or worse (f16: to tens, its values end there): what the running
+    maximum is rounded by must not be an exponent."""
+    def fill(c, ids, q):
+        most = 60000.0 if ty == O.F16 else np.inf
+        q *= size ** 0.5
+        np.clip(q, -most, most, out=q)
+        c.values[0] = np.clip(c.values[0] * size ** 0.5, -most, most)
+    for dim in (64, 128, 256):
+        for new, seed in (([1, 40, 90, 6], 14), (None, 15)):
+            Call(ty, 4, 2, dim, [1, 40, 300, 2100], new=new, seed=seed, fill=fill).check(new is None)
+            Call(ty, 4, 2, dim, [40, 300], new=new and [40, 90], seed=seed, fill=fill).check(new is None)
