@@ -18,7 +18,7 @@ inv_freq[i], and multiplied by a factor that long contexts bring along.
 Sampling, for a row of logits l and T, k, p, m, u (a temperature of 0 takes the largest logit, the first of equals):
 weights exp((l - max l) / T); tokens in order of falling logits, the lower index first among equal ones; kept are the
 first k, of these the smallest head of the order that holds p of their weight, of these the ones with at least m of the
-largest weight, and always the first; then, by index, the first kept token up to which the weights' sum passes u times
+largest weight, and always the first; then, in that order, the first token up to which the weights' sum passes u times
 the sum of all kept ones.  Logits that are NaN or -inf are never taken; a row without another gives -1.
 """
 import math
@@ -416,14 +416,12 @@ def _plain_sample(s):
     keep |= first
     keep &= l > -math.inf
     kept = keep.sum(1)
-    # back to the order of indexes
-    w = torch.zeros_like(w).scatter_(1, order, w * keep)
+    w = w * keep
     c = w.cumsum(1)
     passed = c > s["u"].double()[:, None] * c[:, -1:]
     # (a sum that never passes, by rounding: the last one with a weight)
-    last = x.shape[1] - 1 - (w > 0).flip(1).int().argmax(1)
-    token = torch.where(passed.any(1), passed.int().argmax(1), last)
-    prob = w.gather(1, token[:, None]).squeeze(1) / c[:, -1]
+    at = torch.where(passed.any(1), passed.int().argmax(1), (w > 0).sum(1) - 1).clamp(min=0)[:, None]
+    token, prob = order.gather(1, at).squeeze(1), w.gather(1, at).squeeze(1) / c[:, -1]
     none = kept == 0
     return dict(token=torch.where(none, -torch.ones_like(token), token).int(), kept=kept.int(),
                 prob=torch.where(none, torch.zeros_like(prob), prob).float())
@@ -623,11 +621,9 @@ def _exact_sample(case, s):
             n = max(1, int(np.searchsorted(np.cumsum(w), p * w.sum(), side="left")) + 1)
         if m > 0:
             n = max(1, min(n, int((w >= m).sum())))
-        ids, w = ids[:n], w[:n]
-        by = np.argsort(ids)
-        c = np.cumsum(w[by])
+        c = np.cumsum(w[:n])
         at = min(int(np.searchsorted(c, u[r] * c[-1], side="right")), n - 1)
-        prob[r] = w[by][at] / c[-1]
+        prob[r] = w[at] / c[-1]
     return dict(token=None, kept=None, prob=torch.as_tensor(prob))
 
 
