@@ -114,6 +114,8 @@ enum {
     SAE_ST_SLOT_BUSY = 1u << 4,       /* insert into a valid slot (insert skipped)   */
     SAE_ST_SELECT_FALLBACK = 1u << 5, /* exact slow path of the pool scan was used   */
     SAE_ST_BAD_BLOCK = 1u << 6,       /* block id out of range (element skipped)     */
+    SAE_ST_BAD_TREE = 1u << 8,        /* sae_attn_tree: a parent that is not an earlier
+                                         token, or too many tokens                  */
     SAE_ST_BAD_HASH = 1u << 7         /* a reserved hash (0 or 2^64-1) given to Add()
                                          or found in a valid block by the index build:
                                          that block is skipped (not added, not indexed) */
@@ -655,6 +657,94 @@ sae_status sae_attn_decode(const sae_kv *kv, const sae_seqs *seqs, int32_t n_hea
 sae_status sae_attn_prefill(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t n_heads, int32_t dtype,
                             const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse, float scale,
                             int32_t window, void *work, size_t work_bytes, sae_stream_t stream);
+
+/*
+ * Append: sae_kv_write with the position rotation applied on the way, and the queries
+ * turned beside it.
+ *  rope   turns the first `turned` dimensions of each head (a multiple of 16, 16 ..
+ *         head_dim): pair i < turned / 2, (x, y) at dimensions (i, i + turned / 2), or
+ *         (2 i, 2 i + 1) with interleaved = 1, becomes
+ *           factor (x cos a - y sin a, x sin a + y cos a),  a = position * inv_freq[i]
+ *         (inv_freq: device float [turned / 2]; factor: finite, 1 where there is none); the
+ *         angle is reduced in 64 bits, the rest is fp32, rounded once to the type that is
+ *         stored (an 8-bit cache's scale is found from the turned values)
+ *  pos    device int32 [n_tokens]: each row's position, for rows whose position is not their
+ *         place in the sequence (the tokens of a tree); or NULL: the place
+ *  k, v   as in sae_kv_write; values are stored as they are
+ *  q, q_out  device, [n_tokens][n_heads][head_dim] of `dtype`, strides and alignment as for
+ *         k: the turned queries; may be the same array; n_heads 1 .. 1024, or n_heads = 0 and
+ *         both NULL
+ * A token without a place (see sae_seqs) is not written and its q_out row is zeros; one
+ * whose block is not there is not written.  q_out may not overlap k, v or the cache.
+ */
+typedef struct {
+    const float *inv_freq;
+    float factor;
+    int32_t turned;
+    int32_t interleaved;
+} sae_rope;
+sae_status sae_kv_append(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t n_heads, int32_t dtype,
+                         const sae_rope *rope, const int32_t *pos, const void *q, int64_t q_stride, void *q_out,
+                         int64_t q_out_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                         sae_stream_t stream);
+
+/*
+ * Attention of drafted tokens that form a tree per sequence (or several: a forest) over the cache.
+ * A sequence's new tokens are its tree's nodes, 0 .. n - 1 in the order of their rows and of
+ * their places in the cache (node j at place kv_len - n + j; sae_kv_write or sae_kv_append has
+ * put its key and value there):
+ *  parent[n_tokens]  device int32: each row's parent as a node of its sequence's tree, smaller than
+ *                    the node itself; -1: it follows the cached prefix.  Another value is reported
+ *                    (SAE_ST_BAD_TREE) and taken for -1
+ *  max_nodes         1 .. SAE_TREE_MAX: no sequence has more new tokens (one that does is
+ *                    reported, and its rows see nothing)
+ * A node's position is kv_len - n + its depth.  Its row sees the cached prefix (places before
+ * kv_len - n), its ancestors and itself, with window > 0 those whose position is above its own
+ * minus the window, and where they have a block and a place.  Sums, roundings, rows that see nothing,
+ * values that are not finite, q, out, lse, scale, work and the limit on rows are as in
+ * sae_attn_prefill; a chain (parent[j] = j - 1) gives its results.
+ */
+#define SAE_TREE_MAX 256
+sae_status sae_attn_tree(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, const int32_t *parent, int32_t max_nodes,
+                         int32_t n_heads, int32_t dtype, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                         float *lse, float scale, int32_t window, void *work, size_t work_bytes, sae_stream_t stream);
+
+/*
+ * Sampling: one token per row of logits, from a given random number.
+ *  logits[n_rows][vocab]  device, values of `dtype` (SAE_KV_BF16, SAE_KV_F16 or SAE_ROWS_F32);
+ *                    stride: values from a row to the next one, >= vocab; aligned to a value
+ *  u[n_rows]         device float, 0 <= u < 1 (below 0 or NaN: 0; 1 and above: the last token
+ *                    that has a weight)
+ *  temperature, top_k, top_p, min_p  device [n_rows], or NULL (1, or left out)
+ * With T, k, p, m a row's settings and l its logits, tokens are ordered by falling logit, the
+ * lower index first among equal ones; token i weighs w_i = exp((l_i - l_0) / T), l_0 the largest.
+ * Kept are: the first k (k <= 0: all); of these the shortest head of the order whose weight
+ * is at least p of theirs (p >= 1 or NaN: all); of these the ones with w_i >= m (m <= 0 or NaN: all);
+ * and always the first.  A temperature that is not above 0 keeps the first alone.  The row's
+ * token is the first, in that order, up to which the kept weights' sum passes u times
+ * the sum of all of them.  Logits that are NaN or -inf are not taken; where +inf is the
+ * largest, tokens that have it share the weight evenly.
+ *  token[n_rows]     device int32 out; -1 for a row without a token
+ *  prob[n_rows]      device float out or NULL: the token's share of the kept weights (0 without one)
+ *  kept[n_rows]      device int32 out or NULL: the number of kept tokens
+ *  work              device scratch of at least sae_sample_work_size bytes, 16-byte aligned, as
+ *                    for sae_attn_decode
+ * Weights are computed in 64 bits and summed as whole multiples of 2^-43: results do not depend
+ * on the order of sums or on how rows are divided over the GPU, and a token or a
+ * border is another one than with exact sums only where one lies within vocab * 2^-43 of the other.
+ * Needs 1 <= vocab <= 2^20, 0 <= n_rows <= 2^20.
+ */
+enum { SAE_ROWS_F32 = 3 };
+typedef struct {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p;
+    const float *min_p;
+} sae_sampling;
+sae_status sae_sample_work_size(int32_t n_rows, int32_t vocab, size_t *bytes);
+sae_status sae_sample(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t stride,
+                      const sae_sampling *settings, const float *u, int32_t *token, float *prob, int32_t *kept, void *work,
+                      size_t work_bytes, sae_stream_t stream);
 
 /* Device realisation of the fp32 recipe's elementary functions (the ones
  * Eq. 1 and Eq. 2 are built from), element-wise, for checking it:

@@ -135,3 +135,58 @@ def bounds(out, lse, mag, big, dim, dtype, weight=None, floor=0.0):
     tiny = 2.0 ** -25 if dtype == F16 else 2.0 ** -134  # half the smallest subnormal
     return (u * np.abs(out) + ((u if weight is None else weight) + 2 * rel)[..., None] * mag * (1 + u) + tiny + floor,
             rel + 2.0 ** -22 * np.abs(np.where(np.isfinite(lse), lse, 0)))
+
+
+def tree_seen(parent, total, there, window):
+    """seen [n][total]: which places each node of a tree sees, by walking up from it.  parent [n] (-1: the prefix)."""
+    n = len(parent)
+    base = total - n
+    seen = np.zeros((n, total), bool)
+    for j in range(n):
+        if base + j < 0:
+            continue  # no place
+        way = [j]
+        while parent[way[-1]] >= 0:
+            way.append(parent[way[-1]])
+        pos = base + len(way) - 1
+        for up, i in enumerate(way):
+            if base + i >= 0 and (not window or pos - up > pos - window):
+                seen[j, base + i] = True
+        for t in range(max(base, 0)):
+            if not window or t > pos - window:
+                seen[j, t] = True
+    return seen & there[None, :]
+
+
+def tree_attention(q, parent, k, v, there, scale, window):
+    """Queries q [n][heads][dim] of a tree's nodes, the last n places of keys and values [len][kv_heads][dim]; returns as
+    attention() does."""
+    n, heads, dim = q.shape
+    kvh = k.shape[1]
+    out, mag = np.zeros((n, heads, dim)), np.zeros((n, heads, dim))
+    lse, big = np.full((n, heads), -np.inf), np.zeros((n, heads))
+    seen = tree_seen(parent, k.shape[0], there, window)
+    for i in range(n):
+        at = np.nonzero(seen[i])[0]
+        if not len(at):
+            continue
+        for u in range(heads):
+            kk, vv = k[at, u // (heads // kvh)], v[at, u // (heads // kvh)]
+            s = scale * (kk @ q[i, u])
+            w = np.exp(s - s.max())
+            out[i, u], mag[i, u] = (w @ vv) / w.sum(), (w @ np.abs(vv)) / w.sum()
+            lse[i, u] = s.max() + np.log(w.sum())
+            big[i, u] = abs(scale) * (np.abs(kk) @ np.abs(q[i, u])).max()
+    return out, lse, mag, big
+
+
+def turn(x, pos, inv_freq, interleaved=False, factor=1.0):
+    """Rows x [n][heads][dim] at positions pos [n] turned pair by pair (see sae_rope in include/sae.h)."""
+    half = len(inv_freq)
+    y = np.array(x, np.float64)
+    for i in range(half):
+        a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+        angle = np.asarray(pos, np.float64) * float(inv_freq[i])
+        c, s = factor * np.cos(angle)[:, None], factor * np.sin(angle)[:, None]
+        y[:, :, a], y[:, :, b] = x[:, :, a] * c - x[:, :, b] * s, x[:, :, a] * s + x[:, :, b] * c
+    return y

@@ -100,6 +100,20 @@ class SaeSeqs(ctypes.Structure):
     ]
 
 
+class SaeRope(ctypes.Structure):
+    device = None
+    _fields_ = [
+        ("inv_freq", ctypes.c_void_p),
+        ("factor", ctypes.c_float),
+        ("turned", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+    ]
+
+
+class SaeSampling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
 # exported symbol -> (restype, argtypes)
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -142,6 +156,11 @@ SIGNATURES = {
     "sae_attn_work_size": (_I32, [_KV, _SQ, _I32, _I32, ctypes.POINTER(_SZ)]),
     "sae_attn_decode": (_I32, [_KV, _SQ, _I32, _I32, _P, _I64, _P, _I64, _P, _F32, _I32, _P, _SZ, _P]),
     "sae_attn_prefill": (_I32, [_KV, _SQ, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _F32, _I32, _P, _SZ, _P]),
+    "sae_kv_append": (_I32, [_KV, _SQ, _I32, _I32, _I32, ctypes.POINTER(SaeRope), _P, _P, _I64, _P, _I64, _P, _I64, _P, _I64,
+                             _P]),
+    "sae_attn_tree": (_I32, [_KV, _SQ, _I32, _P, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _F32, _I32, _P, _SZ, _P]),
+    "sae_sample_work_size": (_I32, [_I32, _I32, ctypes.POINTER(_SZ)]),
+    "sae_sample": (_I32, [_I32, _I32, _I32, _P, _I64, ctypes.POINTER(SaeSampling), _P, _P, _P, _P, _P, _SZ, _P]),
     "sae_select_stats": (_I32, [_P, _I32, _P, _P]),
     "sae_profile_enable": (_I32, [_P, _I32]),
     "sae_profile_read": (_I32, [_P, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_I64)]),

@@ -9,7 +9,7 @@ import ctypes
 import torch
 
 from . import _lib
-from ._lib import IVL_CAP, N_BINS, SaeConfig, SaeCounters, SaeError, SaeKv, SaeParams, SaePool, SaePredictor, SaeSeqs  # noqa: F401
+from ._lib import IVL_CAP, N_BINS, SaeConfig, SaeCounters, SaeError, SaeKv, SaeParams, SaePool, SaePredictor, SaeRope, SaeSampling, SaeSeqs  # noqa: F401
 
 KIND_EVICT_FIRST, KIND_STRUCTURAL, KIND_LOGNORMAL, KIND_RECENCY = 0, 1, 2, 3
 META_VALID, META_LEAF, META_REF = 0x40, 0x80, 0x100
@@ -23,7 +23,7 @@ LEARN_TOKEN_EMA, LEARN_QUEUE_REL = 16, 32
 # the paper's initial token weights (system, user, tool, response, cot), Sec. 5
 PAPER_INIT_W = (2.0, 1.5, 1.0, 1.0, 0.1)
 ST_NAMES = {1: "INDEX_FULL", 2: "GHOST_FULL", 4: "BAD_OFFSET", 8: "FUTURE_ACCESS",
-            16: "SLOT_BUSY", 32: "SELECT_FALLBACK", 64: "BAD_BLOCK", 128: "BAD_HASH"}
+            16: "SLOT_BUSY", 32: "SELECT_FALLBACK", 64: "BAD_BLOCK", 128: "BAD_HASH", 256: "BAD_TREE"}
 
 
 def _ptr(t):
@@ -486,6 +486,123 @@ def sae_attn_prefill(kv, seqs, q, out, scale, work, window=0, lse=None, stream=N
     n, heads, ty, qp, qs, op, os_, lp, wp, wn = _attn_rows(kv, q, out, lse, work)
     st = _lib.load().sae_attn_prefill(ctypes.byref(kv), ctypes.byref(seqs), n, heads, ty, qp, qs, op, os_, lp, scale,
                                       window, wp, wn, _raw_stream(kv, seqs, q, out, lse, work, stream))
+    if st:
+        _check(None, st)
+
+
+TREE_MAX = 256
+
+
+def sae_attn_tree(kv, seqs, parent, max_nodes, q, out, scale, work, window=0, lse=None, stream=None):
+    """Attention of drafted tokens that form a tree per sequence over its cache and themselves: q, out
+    [n_tokens][heads][head_dim], parent int32 [n_tokens] (see include/sae.h); no sequence has more than max_nodes."""
+    n, heads, ty, qp, qs, op, os_, lp, wp, wn = _attn_rows(kv, q, out, lse, work)
+    if parent.dtype != torch.int32 or parent.numel() != n:
+        raise SaeError("parent must be int32 with %d elements" % n)
+    pp = _ptr(parent)
+    handle = _raw_stream(kv, seqs, q, out, lse, work, stream)
+    if parent.get_device() != torch._C._cuda_getDevice():
+        raise SaeError("a call's tensors must all be on the current device")
+    st = _lib.load().sae_attn_tree(ctypes.byref(kv), ctypes.byref(seqs), n, pp, max_nodes, heads, ty, qp, qs, op, os_, lp,
+                                   scale, window, wp, wn, handle)
+    if st:
+        _check(None, st)
+
+
+def make_rope(inv_freq, interleaved=False, factor=1.0):
+    """The position rotation of sae_kv_append: turns 2 len(inv_freq) dimensions of each head (see sae_rope in
+    include/sae.h); it keeps the tensor alive."""
+    if inv_freq.dtype != torch.float32:
+        raise SaeError("inv_freq must be float32")
+    r = SaeRope()
+    r.inv_freq, r.factor = _ptr(inv_freq).value, float(factor)
+    r.turned, r.interleaved = 2 * inv_freq.numel(), 1 if interleaved else 0
+    r.tensors, r.device = (inv_freq,), inv_freq.get_device()
+    return r
+
+
+def sae_kv_append(kv, seqs, rope, q, q_out, k, v, pos=None, stream=None):
+    """sae_kv_write with keys and queries [n_tokens][heads][head_dim] turned by their positions (pos int32 [n_tokens], or
+    their places) on the way; the turned queries go to q_out, which may be q (both None: no queries)."""
+    heads, dim = kv.n_kv_heads, kv.head_dim
+    kp, ks, kt, n = _rows(k, heads, dim)
+    vp, vs, vt, vn = _rows(v, heads, dim)
+    if kt != vt or n != vn:
+        raise SaeError("k and v must have one type and one length")
+    qp = op = None
+    qs = os_ = qh = 0
+    if q is not None or q_out is not None:
+        if q is None or q_out is None:
+            raise SaeError("q and q_out go together")
+        qh = q.shape[1] if q.dim() == 3 else 0
+        qp, qs, qt, qn = _rows(q, qh, dim)
+        op, os_, ot, on = _rows(q_out, qh, dim)
+        if (qt, qn) != (kt, n) or (ot, on) != (kt, n):
+            raise SaeError("q and q_out must have k's type and length")
+    pp = None
+    if pos is not None:
+        if pos.dtype != torch.int32 or pos.numel() != n:
+            raise SaeError("pos must be int32 with %d elements" % n)
+        pp = _ptr(pos)
+    handle = _raw_stream(kv, seqs, k, v, q, q_out, stream)
+    here = torch._C._cuda_getDevice()
+    if (pos is not None and pos.get_device() != here) or rope.device not in (here, None):
+        raise SaeError("a call's tensors must all be on the current device (%d)" % here)
+    st = _lib.load().sae_kv_append(ctypes.byref(kv), ctypes.byref(seqs), n, qh, kt, ctypes.byref(rope), pp, qp, qs, op, os_,
+                                   kp, ks, vp, vs, handle)
+    if st:
+        _check(None, st)
+
+
+# --------------------------------------------------------------- sampling
+ROWS_F32 = 3
+_LOGITS = {torch.bfloat16: KV_BF16, torch.float16: KV_F16, torch.float32: ROWS_F32}
+
+
+def sae_sample_work_size(n_rows, vocab):
+    """Bytes of device scratch that a sampling call of this size needs."""
+    n = ctypes.c_size_t()
+    _check(None, _lib.load().sae_sample_work_size(int(n_rows), int(vocab), ctypes.byref(n)))
+    return n.value
+
+
+def sae_sample(logits, u, token, work, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, kept=None,
+               stream=None):
+    """A token per row of logits [n][vocab] (bf16, f16 or float32; rows may lie apart) from random numbers u [n] in [0, 1):
+    token int32 [n].  temperature, top_p, min_p float32 and top_k int32, [n] each or None (see include/sae.h); prob float32
+    and kept int32 [n] receive the token's share and the number of tokens that could be drawn."""
+    if not logits.is_cuda:
+        raise SaeError("expected a device tensor")
+    if logits.dim() != 2 or logits.dtype not in _LOGITS:
+        raise SaeError("logits must be [n][vocab] of bfloat16, float16 or float32")
+    n, vocab = logits.shape
+    if n and vocab > 1 and logits.stride(1) != 1:
+        raise SaeError("a row of logits must be contiguous")
+    here = torch._C._cuda_getDevice()
+    if logits.get_device() != here or work.get_device() != here:
+        raise SaeError("a call's tensors must all be on the current device (%d)" % here)
+    p = []
+    for name, t, dtype in (("u", u, torch.float32), ("token", token, torch.int32), ("temperature", temperature, torch.float32),
+                           ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32),
+                           ("prob", prob, torch.float32), ("kept", kept, torch.int32)):
+        if t is None:
+            p.append(None)
+            continue
+        if t.dtype != dtype or t.numel() != n:
+            raise SaeError("%s must be %s with %d elements" % (name, str(dtype)[6:], n))
+        if t.get_device() != here:
+            raise SaeError("a call's tensors must all be on the current device (%d)" % here)
+        p.append(_ptr(t).value)
+    s = SaeSampling(*p[2:6])
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(here)
+    elif stream.device_index != here:
+        raise SaeError("the stream must be on the current device (%d), it is on %d" % (here, stream.device_index))
+    else:
+        handle = stream.cuda_stream
+    st = _lib.load().sae_sample(n, vocab, _LOGITS[logits.dtype], logits.data_ptr(), logits.stride(0) if n > 1 else vocab,
+                                ctypes.byref(s), p[0], p[1], p[6], p[7], _ptr(work), work.numel() * work.element_size(),
+                                handle)
     if st:
         _check(None, st)
 

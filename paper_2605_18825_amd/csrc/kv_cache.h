@@ -79,6 +79,17 @@ hipError_t launch_kv_write(const KvDev &c, int type, int dim, int dtype, const v
 hipError_t launch_kv_read(const KvDev &c, int type, int dim, int dtype, void *k, int64_t k_stride, void *v,
                           int64_t v_stride, hipStream_t s);
 
+// An append, checked.  Strides in values; q and q_out may be null together.
+struct AppendArgs {
+    const sae_rope *rope;
+    const int32_t *pos;
+    int32_t heads;
+    const void *q, *k, *v;
+    void *q_out;
+    int64_t q_stride, out_stride, k_stride, v_stride;
+};
+hipError_t launch_kv_append(const KvDev &c, int type, int dim, int dtype, const AppendArgs &x, hipStream_t s);
+
 // One attention call, checked.  Strides in values.
 struct AttnArgs {
     const void *q;
@@ -88,9 +99,26 @@ struct AttnArgs {
     float scale;
     int32_t window, heads;
     void *work;
+    // sae_attn_tree only
+    const int32_t *parent;
+    int32_t max_nodes;
 };
 hipError_t launch_decode(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s);
+hipError_t launch_tree(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s);
 hipError_t launch_prefill(const KvDev &c, const AttnArgs &a, int type, int dim, hipStream_t s);
+// A sampling call, checked.
+struct SampleArgs {
+    const void *logits;
+    int64_t stride;
+    sae_sampling settings;
+    const float *u;
+    int32_t *token, *kept;
+    float *prob;
+    void *work;
+};
+hipError_t launch_sample(int rows, int vocab, int dtype, const SampleArgs &x, hipStream_t s);
+size_t sample_work_bytes(int rows, int vocab);
+
 size_t decode_work_bytes(int heads, int kvh, int dim);
 size_t prefill_work_bytes(int kvh, int dim);
 bool prefill_fits(const KvDev &c, int heads);

@@ -630,6 +630,35 @@ sae_status sae_kv_read(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
     return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, "sae_kv_read");
 }
 
+sae_status sae_kv_append(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, int32_t n_heads, int32_t dtype,
+                         const sae_rope *rope, const int32_t *pos, const void *q, int64_t q_stride, void *q_out,
+                         int64_t q_out_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                         sae_stream_t stream)
+{
+    auto bad = [](const char *msg) { return fail(nullptr, SAE_ERR_ARG, msg); };
+    KvDev d;
+    sae_status st = kv_move_args(kv, seqs, n_tokens, dtype, k, k_stride, v, v_stride, d);
+    if (st != SAE_OK) return st;
+    if (!rope || !rope->inv_freq || !aligned(rope->inv_freq, 4)) return bad("rope and its inv_freq must be non-NULL, inv_freq 4-byte aligned");
+    if (rope->turned < 16 || rope->turned > kv->head_dim || rope->turned % 16 != 0)
+        return bad("rope: turned must be a multiple of 16 in 16..head_dim");
+    if (rope->interleaved != 0 && rope->interleaved != 1) return bad("rope: interleaved must be 0 or 1");
+    if (!(rope->factor - rope->factor == 0.0f)) return bad("rope: factor must be finite");
+    if (!aligned(pos, 4)) return bad("pos must be 4-byte aligned");
+    const bool queries = q || q_out || n_heads != 0;
+    if (queries && n_tokens > 0) {
+        if (n_heads < 1 || n_heads > 1024) return bad("n_heads must be in 1..1024, or 0 without queries");
+        const int64_t row = (int64_t)n_heads * kv->head_dim;
+        const char *msg = rows_args(q, q_stride, row);
+        if (!msg) msg = rows_args(q_out, q_out_stride, row);
+        if (msg) return bad(msg);
+    }
+    if (n_tokens == 0) return SAE_OK;
+    const AppendArgs a = {rope, pos, n_heads, q, k, v, q_out, q_stride, q_out_stride, k_stride, v_stride};
+    hipError_t e = launch_kv_append(d, kv->type, kv->head_dim, dtype, a, S(stream));
+    return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, "sae_kv_append");
+}
+
 static size_t attn_work_bytes(int heads, int kvh, int dim)
 {
     const size_t d = decode_work_bytes(heads, kvh, dim), p = prefill_work_bytes(kvh, dim);
@@ -655,9 +684,12 @@ sae_status sae_attn_work_size(const sae_kv *kv, const sae_seqs *seqs, int32_t n_
     return SAE_OK;
 }
 
-static sae_status attn(const char *name, bool decode, const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
+enum class Attn { DECODE, PREFILL, TREE };
+
+static sae_status attn(const char *name, Attn kind, const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens,
                        int32_t n_heads, int32_t dtype, const void *q, int64_t q_stride, void *out, int64_t out_stride,
-                       float *lse, float scale, int32_t window, void *work, size_t work_bytes, hipStream_t s)
+                       float *lse, float scale, int32_t window, void *work, size_t work_bytes, hipStream_t s,
+                       const int32_t *parent = nullptr, int32_t max_nodes = 0)
 {
     KvDev d;
     sae_status st = kv_args(kv, seqs, n_tokens, d);
@@ -667,21 +699,26 @@ static sae_status attn(const char *name, bool decode, const sae_kv *kv, const sa
         return fail(nullptr, SAE_ERR_ARG, "dtype must be the cache's type, bf16 for an FP8 cache");
     if (!(scale - scale == 0.0f)) return fail(nullptr, SAE_ERR_ARG, "scale must be finite");
     if (window < 0) return fail(nullptr, SAE_ERR_ARG, "window must be >= 0");
+    if (kind == Attn::TREE && (max_nodes < 1 || max_nodes > SAE_TREE_MAX)) return fail(nullptr, SAE_ERR_ARG, "max_nodes must be in 1..256");
     if (n_tokens == 0) return SAE_OK;
+    if (kind == Attn::TREE && (!parent || !aligned(parent, 4)))
+        return fail(nullptr, SAE_ERR_ARG, "parent must be non-NULL and 4-byte aligned");
     const int64_t row = (int64_t)n_heads * kv->head_dim;
     const char *msg = rows_args(q, q_stride, row);
     if (!msg) msg = rows_args(out, out_stride, row);
     if (msg) return fail(nullptr, SAE_ERR_ARG, msg);
     if (!aligned(lse, 4)) return fail(nullptr, SAE_ERR_ARG, "lse must be 4-byte aligned");
-    if (!decode && !prefill_fits(d, n_heads))
+    if (kind != Attn::DECODE && !prefill_fits(d, n_heads))
         return fail(nullptr, SAE_ERR_ARG, "too many rows for one call: n_tokens * n_heads / 128 + n_seq * n_kv_heads >= 2^23");
     if (!work || !aligned(work, 16) || work_bytes < attn_work_bytes(n_heads, kv->n_kv_heads, kv->head_dim))
         return fail(nullptr, SAE_ERR_ARG, "work must be 16-byte aligned and hold sae_attn_work_size bytes");
     // No position reaches past the table: a longer window is that long (then no difference of
     // a position, which may be as low as -n_tokens, and the window passes 32 bits).
     const int32_t most = seqs->max_blocks * SAE_KV_BLOCK;
-    const AttnArgs a = {q, out, lse, q_stride, out_stride, scale, window < most ? window : most, n_heads, work};
-    hipError_t e = (decode ? launch_decode : launch_prefill)(d, a, kv->type, kv->head_dim, s);
+    const AttnArgs a = {q, out, lse, q_stride, out_stride, scale, window < most ? window : most, n_heads, work,
+                        parent, max_nodes};
+    auto launch = kind == Attn::DECODE ? launch_decode : kind == Attn::PREFILL ? launch_prefill : launch_tree;
+    hipError_t e = launch(d, a, kv->type, kv->head_dim, s);
     return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, name);
 }
 
@@ -690,7 +727,7 @@ sae_status sae_attn_decode(const sae_kv *kv, const sae_seqs *seqs, int32_t n_hea
                            void *work, size_t work_bytes, sae_stream_t stream)
 {
     if (seqs && seqs->q_start) return fail(nullptr, SAE_ERR_ARG, "sae_attn_decode takes no q_start");
-    return attn("sae_attn_decode", true, kv, seqs, seqs ? seqs->n_seq : 0, n_heads, dtype, q, q_stride, out, out_stride,
+    return attn("sae_attn_decode", Attn::DECODE, kv, seqs, seqs ? seqs->n_seq : 0, n_heads, dtype, q, q_stride, out, out_stride,
                 lse, scale, window, work, work_bytes, S(stream));
 }
 
@@ -698,8 +735,55 @@ sae_status sae_attn_prefill(const sae_kv *kv, const sae_seqs *seqs, int32_t n_to
                             const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse, float scale,
                             int32_t window, void *work, size_t work_bytes, sae_stream_t stream)
 {
-    return attn("sae_attn_prefill", false, kv, seqs, n_tokens, n_heads, dtype, q, q_stride, out, out_stride, lse, scale,
+    return attn("sae_attn_prefill", Attn::PREFILL, kv, seqs, n_tokens, n_heads, dtype, q, q_stride, out, out_stride, lse, scale,
                 window, work, work_bytes, S(stream));
+}
+
+sae_status sae_attn_tree(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, const int32_t *parent, int32_t max_nodes,
+                         int32_t n_heads, int32_t dtype, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                         float *lse, float scale, int32_t window, void *work, size_t work_bytes, sae_stream_t stream)
+{
+    return attn("sae_attn_tree", Attn::TREE, kv, seqs, n_tokens, n_heads, dtype, q, q_stride, out, out_stride, lse, scale,
+                window, work, work_bytes, S(stream), parent, max_nodes);
+}
+
+static sae_status sample_size(int32_t n_rows, int32_t vocab)
+{
+    if (n_rows < 0 || n_rows > (1 << 20)) return fail(nullptr, SAE_ERR_ARG, "n_rows must be in 0..2^20");
+    if (vocab < 1 || vocab > (1 << 20)) return fail(nullptr, SAE_ERR_ARG, "vocab must be in 1..2^20");
+    return SAE_OK;
+}
+
+sae_status sae_sample_work_size(int32_t n_rows, int32_t vocab, size_t *bytes)
+{
+    sae_status st = sample_size(n_rows, vocab);
+    if (st != SAE_OK) return st;
+    if (!bytes) return fail(nullptr, SAE_ERR_ARG, "bytes must be non-NULL");
+    *bytes = sample_work_bytes(n_rows, vocab);
+    return SAE_OK;
+}
+
+sae_status sae_sample(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t stride,
+                      const sae_sampling *settings, const float *u, int32_t *token, float *prob, int32_t *kept, void *work,
+                      size_t work_bytes, sae_stream_t stream)
+{
+    auto bad = [](const char *msg) { return fail(nullptr, SAE_ERR_ARG, msg); };
+    sae_status st = sample_size(n_rows, vocab);
+    if (st != SAE_OK) return st;
+    if (dtype != SAE_KV_BF16 && dtype != SAE_KV_F16 && dtype != SAE_ROWS_F32) return bad("dtype must be bf16, f16 or f32");
+    if (stride < vocab || stride > (1ll << 38)) return bad("stride must hold a row of vocab values");
+    if (n_rows == 0) return SAE_OK;
+    if (!logits || !aligned(logits, dtype == SAE_ROWS_F32 ? 4 : 2)) return bad("logits must be non-NULL and aligned to a value");
+    if (!u || !token) return bad("u and token must be non-NULL");
+    const sae_sampling s = settings ? *settings : sae_sampling{};
+    if (!aligned(u, 4) || !aligned(token, 4) || !aligned(prob, 4) || !aligned(kept, 4) || !aligned(s.temperature, 4) ||
+        !aligned(s.top_k, 4) || !aligned(s.top_p, 4) || !aligned(s.min_p, 4))
+        return bad("u, token, prob, kept and the settings must be 4-byte aligned");
+    if (!work || !aligned(work, 16) || work_bytes < sample_work_bytes(n_rows, vocab))
+        return bad("work must be 16-byte aligned and hold sae_sample_work_size bytes");
+    const SampleArgs a = {logits, stride, s, u, token, kept, prob, work};
+    hipError_t e = launch_sample(n_rows, vocab, dtype, a, S(stream));
+    return e == hipSuccess ? SAE_OK : hip_fail(nullptr, e, "sae_sample");
 }
 
 sae_status sae_block_type(const uint8_t *counts, int64_t n, uint8_t *tau, sae_stream_t stream)
