@@ -566,6 +566,19 @@ def sae_sample_work_size(n_rows, vocab):
     return n.value
 
 
+def _vector(name, t, dtype, n, here):
+    """Address of a row's settings or results, n values of `dtype` on the current device; None for none."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n:
+        raise SaeError("%s must be %s with %d elements" % (name, str(dtype)[6:], n))
+    if t.get_device() != here:
+        raise SaeError("a call's tensors must all be on the current device (%d)" % here)
+    if not t.is_contiguous():
+        raise SaeError("expected a contiguous tensor")
+    return t.data_ptr()
+
+
 def sae_sample(logits, u, token, work, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, kept=None,
                stream=None):
     """A token per row of logits [n][vocab] (bf16, f16 or float32; rows may lie apart) from random numbers u [n] in [0, 1):
@@ -573,36 +586,29 @@ def sae_sample(logits, u, token, work, temperature=None, top_k=None, top_p=None,
     and kept int32 [n] receive the token's share and the number of tokens that could be drawn."""
     if not logits.is_cuda:
         raise SaeError("expected a device tensor")
-    if logits.dim() != 2 or logits.dtype not in _LOGITS:
+    ty = _LOGITS.get(logits.dtype)
+    if ty is None or logits.dim() != 2:
         raise SaeError("logits must be [n][vocab] of bfloat16, float16 or float32")
     n, vocab = logits.shape
-    if n and vocab > 1 and logits.stride(1) != 1:
+    stride, step = logits.stride()
+    if n and vocab > 1 and step != 1:
         raise SaeError("a row of logits must be contiguous")
     here = torch._C._cuda_getDevice()
     if logits.get_device() != here or work.get_device() != here:
         raise SaeError("a call's tensors must all be on the current device (%d)" % here)
-    p = []
-    for name, t, dtype in (("u", u, torch.float32), ("token", token, torch.int32), ("temperature", temperature, torch.float32),
-                           ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32),
-                           ("prob", prob, torch.float32), ("kept", kept, torch.int32)):
-        if t is None:
-            p.append(None)
-            continue
-        if t.dtype != dtype or t.numel() != n:
-            raise SaeError("%s must be %s with %d elements" % (name, str(dtype)[6:], n))
-        if t.get_device() != here:
-            raise SaeError("a call's tensors must all be on the current device (%d)" % here)
-        p.append(_ptr(t).value)
-    s = SaeSampling(*p[2:6])
+    f32, i32 = torch.float32, torch.int32
+    settings = SaeSampling(_vector("temperature", temperature, f32, n, here), _vector("top_k", top_k, i32, n, here),
+                           _vector("top_p", top_p, f32, n, here), _vector("min_p", min_p, f32, n, here))
+    up, tp = _vector("u", u, f32, n, here), _vector("token", token, i32, n, here)
+    pp, kp = _vector("prob", prob, f32, n, here), _vector("kept", kept, i32, n, here)
     if stream is None:
         handle = torch._C._cuda_getCurrentRawStream(here)
     elif stream.device_index != here:
         raise SaeError("the stream must be on the current device (%d), it is on %d" % (here, stream.device_index))
     else:
         handle = stream.cuda_stream
-    st = _lib.load().sae_sample(n, vocab, _LOGITS[logits.dtype], logits.data_ptr(), logits.stride(0) if n > 1 else vocab,
-                                ctypes.byref(s), p[0], p[1], p[6], p[7], _ptr(work), work.numel() * work.element_size(),
-                                handle)
+    st = _lib.load().sae_sample(n, vocab, ty, logits.data_ptr(), stride if n > 1 else vocab, settings, up, tp, pp, kp,
+                                _ptr(work), work.numel() * work.element_size(), handle)
     if st:
         _check(None, st)
 

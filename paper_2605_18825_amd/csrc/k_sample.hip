@@ -6,28 +6,30 @@
 // exp((l - l_0) / T) are computed in 64 bits and held as whole multiples of 2^-43 (the sum of 2^20
 // fits 64 bits): sums are exact, whatever their order, and LDS atomics can take them.
 //
-// A workgroup takes a row.
+// A workgroup takes a row.  The first pass finds the maximum, and each thread keeps the maxima of 16
+// groups of its logits: a later pass for the few largest logits reads those groups alone.
 //   small k     the k-th largest of the threads' maxima bounds the k-th largest logit from below:
-//               one more pass collects what is not below it, a few more than k tokens.
-//   otherwise   a histogram over (l_0 - l) / T, 64 bins per unit, holds each bin's tokens and
-//               weight; the answers' bin follows from it, and one more pass collects the tokens up
-//               to that bin.
+//               what is not below it is collected, a few more than k tokens.
+//   otherwise   a second pass adds every token to a histogram over (l_0 - l) / T, 32 bins for a
+//               factor of two: each bin's tokens and their weight.  The answers' bin follows, and
+//               the tokens up to it are collected.
 //   where these are more than LDS holds, each question is answered by itself: its bin, then
-//   (a bin of many equal or near logits) 11 bits of the logit at a time, then the index.
+//   (a bin of many equal or near logits) 10 bits of the logit at a time, then the index.
 #include "attn_tile.h"
 
 namespace {
 
-using attn::scan;
 using attn::uniform;
 
-constexpr int NW = 16, THREADS = NW * SAE_WAVE;
 constexpr int LIST = 2048;           // tokens that are sorted in LDS
-constexpr int BINS = 2048;           // of a histogram; the last one's tokens weigh nothing
-constexpr float PER_UNIT = 64.0f;    // bins of a unit of (l_0 - l) / T: 2047 / 64 = 32 units, e^-32 = 2^-46
-constexpr int SMALL_K = 256;         // threads' maxima bound the k-th logit
+constexpr int PER_TWO = 32;          // bins of a factor of two in weight
+constexpr int LIGHT = 47 * PER_TWO;  // the bin of tokens that weigh less than half a unit, as nothing
+constexpr int BINS = 1536, DIGITS = 1024;
+constexpr int GROUPS = 16;           // of a thread's logits
 constexpr double ONE = 8796093022208.0;  // 2^43
+constexpr float LOWEST = -__builtin_inff();
 typedef unsigned long long u64;
+static_assert(LIGHT < BINS, "");
 
 struct Args {
     const void *logits;
@@ -39,71 +41,40 @@ struct Args {
     int32_t vocab;
 };
 
-// Ascending whole numbers for falling logits.
-__device__ __forceinline__ uint32_t key_of(float l)
+// ------------------------------------------------------------- waves and workgroups
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ uint32_t moved(uint32_t idle, uint32_t x)
 {
-    const uint32_t b = __float_as_uint(l + 0.0f);  // (-0 and 0 are equal)
-    return b >> 31 ? b : ~b & 0x7FFFFFFFu;
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)idle, (int)x, CTRL, ROWS, 0xF, false);
 }
-__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key >> 31 ? key : ~key & 0x7FFFFFFFu); }
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ u64 moved(u64 idle, u64 x)
+{
+    return (u64)moved<CTRL, ROWS>((uint32_t)(idle >> 32), (uint32_t)(x >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)idle, (uint32_t)x);
+}
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ float moved(float idle, float x)
+{
+    return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(idle), __float_as_uint(x)));
+}
 
-template <int DT>
-struct Row {
-    static constexpr int E = DT == SAE_ROWS_F32 ? 4 : 8;  // logits of 16 bytes
-    static constexpr int SIZE = 16 / E;
-    const char *at;
-    int n, head, vectors;  // logits before the first 16-byte boundary, whole vectors behind them
-
-    __device__ __forceinline__ Row(const void *p, int vocab) : at(static_cast<const char *>(p)), n(vocab)
-    {
-        head = min((int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / SIZE, n);
-        vectors = (n - head) / E;
-    }
-    static __device__ __forceinline__ float wide(u32x4 x, int i)
-    {
-        if constexpr (DT == SAE_ROWS_F32) return __uint_as_float(x[i]);
-        else return i & 1 ? attn::high<DT == SAE_KV_F16>(x[i / 2]) : attn::low<DT == SAE_KV_F16>(x[i / 2]);
-    }
-    __device__ __forceinline__ float one(int i) const
-    {
-        if constexpr (DT == SAE_ROWS_F32) return reinterpret_cast<const float *>(at)[i];
-        else return attn::low<DT == SAE_KV_F16>((uint32_t)reinterpret_cast<const uint16_t *>(at)[i]);
-    }
-    // f(logit, index) for every logit, by the whole workgroup.
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const
-    {
-        constexpr int UN = 4;
-        const char *body = at + (int64_t)head * SIZE;
-        const int t = threadIdx.x;
-#pragma unroll 1
-        for (int v = t; v < vectors; v += THREADS * UN) {
-            u32x4 x[UN];
-#pragma unroll
-            for (int k = 0; k < UN; ++k) {
-                const int w = min(v + k * THREADS, vectors - 1);
-                x[k] = *reinterpret_cast<const u32x4 *>(body + (int64_t)w * 16);
-            }
-#pragma unroll
-            for (int k = 0; k < UN; ++k)
-                if (v + k * THREADS < vectors) {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) f(wide(x[k], i), head + (v + k * THREADS) * E + i);
-                }
-        }
-        const int tail = n - head - vectors * E;  // fewer than E, as the head's
-        if (t < head) f(one(t), t);
-        else if (t >= SAE_WAVE && t < SAE_WAVE + tail) f(one(n - tail + t - SAE_WAVE), n - tail + t - SAE_WAVE);
-    }
-};
-
+// f over lanes 0 .. this one, by moves within rows of 16 lanes and from row to row; `idle` changes nothing.
 template <typename T, typename F>
-__device__ __forceinline__ T over_wave(T x, F f)
+__device__ __forceinline__ T upto(T x, T idle, F f)
 {
-#pragma unroll
-    for (int o = 1; o < SAE_WAVE; o <<= 1) x = f(x, __shfl_xor(x, o));
-    return x;
+    x = f(x, moved<0x111>(idle, x));        // row_shr 1, 2, 4, 8
+    x = f(x, moved<0x112>(idle, x));
+    x = f(x, moved<0x114>(idle, x));
+    x = f(x, moved<0x118>(idle, x));
+    x = f(x, moved<0x142, 0xA>(idle, x));   // the rows' last lanes into the rows behind
+    return f(x, moved<0x143, 0xC>(idle, x));
 }
+template <typename T>
+__device__ __forceinline__ T sum_upto(T x) { return upto(x, (T)0, [](T a, T b) { return a + b; }); }
+
+__device__ __forceinline__ uint32_t of_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ __forceinline__ u64 of_lane(u64 x, int lane) { return (u64)of_lane((uint32_t)(x >> 32), lane) << 32 | of_lane((uint32_t)x, lane); }
+__device__ __forceinline__ float of_lane(float x, int lane) { return __uint_as_float(of_lane(__float_as_uint(x), lane)); }
 
 struct Hist {
     u64 mass[BINS];
@@ -112,97 +83,261 @@ struct Hist {
 
 struct Shared {
     Hist bins;
-    union {           // (digits are done with when a list is summed)
-        Hist digits;
+    union {  // (digits are done with when a list is summed)
+        struct {
+            u64 mass[DIGITS];
+            uint32_t count[DIGITS];
+        } digits;
         u64 sums[LIST];  // weights up to each token of the list, itself included
     };
-    u64 list[LIST];   // key << 32 | index
-    u64 tmp[NW];
-    uint32_t tmp32[NW];
-    uint32_t n, found;
+    u64 list[LIST];  // key << 32 | index
+    double power[PER_TWO];  // 2^(-j / 32) units
+    u64 part[2][16];
+    uint32_t n, found, want;
+};
+
+// f over the workgroup, in every thread; which: alternates between calls.
+template <int NW, typename T, typename F>
+__device__ __forceinline__ T over_all(Shared &s, int which, T x, T idle, F f)
+{
+    T *part = reinterpret_cast<T *>(s.part[which]);
+    x = upto(x, idle, f);
+    if (__lane_id() == SAE_WAVE - 1) part[threadIdx.x / SAE_WAVE] = x;
+    __syncthreads();
+    x = part[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) x = f(x, part[w]);
+    return x;
+}
+
+// The sum over the threads before this one; which: alternates between calls.
+template <int NW, typename T>
+__device__ __forceinline__ T sum_before(Shared &s, int which, T x)
+{
+    T *part = reinterpret_cast<T *>(s.part[which]);
+    const T mine = sum_upto(x);
+    if (__lane_id() == SAE_WAVE - 1) part[threadIdx.x / SAE_WAVE] = mine;
+    __syncthreads();
+    T before = mine - x;
+#pragma unroll
+    for (int w = 0; w < NW - 1; ++w)
+        if (w < (int)threadIdx.x / SAE_WAVE) before += part[w];
+    return before;
+}
+
+// ------------------------------------------------------------- a row
+// Ascending whole numbers for falling logits.
+__device__ __forceinline__ uint32_t key_of(float l)
+{
+    const uint32_t b = __float_as_uint(l + 0.0f);  // (-0 and 0 are equal)
+    return b >> 31 ? b : ~b & 0x7FFFFFFFu;
+}
+__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key >> 31 ? key : ~key & 0x7FFFFFFFu); }
+
+template <int DT, int THREADS>
+struct Row {
+    static constexpr int E = DT == SAE_ROWS_F32 ? 4 : 8;  // logits of 16 bytes
+    static constexpr int SIZE = 16 / E, UN = 4;
+    const char *at, *body;
+    int n, head, vectors;  // logits before the first 16-byte boundary, whole vectors behind them
+    bool infinite;         // +inf is the largest: it counts as 0 then, and other logits as -2^127
+    float most[GROUPS];    // maxima of the thread's groups: group g has vectors (16 i + g) THREADS + thread
+    float edge;            // the thread's logit before or behind the vectors, and its index
+    int edge_at;
+
+    __device__ __forceinline__ Row(const void *p, int vocab) : at(static_cast<const char *>(p)), n(vocab), infinite(false)
+    {
+        head = min((int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / SIZE, n);
+        vectors = (n - head) / E;
+        body = at + head * SIZE;
+        const int t = threadIdx.x, tail = n - head - vectors * E;  // both below E
+        edge_at = t < head ? t : t >= SAE_WAVE && t < SAE_WAVE + tail ? n - tail + t - SAE_WAVE : -1;
+    }
+    __device__ __forceinline__ float mapped(float l) const
+    {
+        return infinite ? (l == __builtin_inff() ? 0.0f : l > LOWEST ? -0x1p127f : LOWEST) : l;
+    }
+    static __device__ __forceinline__ float wide(u32x4 x, int i)
+    {
+        if constexpr (DT == SAE_ROWS_F32) return __uint_as_float(x[i]);
+        else return i & 1 ? attn::high<DT == SAE_KV_F16>(x[i / 2]) : attn::low<DT == SAE_KV_F16>(x[i / 2]);
+    }
+    __device__ __forceinline__ u32x4 vector(int v) const { return *reinterpret_cast<const u32x4 *>(body + (int64_t)v * 16); }
+
+    // The first pass: the thread's maxima; returns the largest.
+    __device__ __forceinline__ float maxima()
+    {
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) most[g] = LOWEST;
+        edge = LOWEST;
+        if (edge_at >= 0) {
+            if constexpr (DT == SAE_ROWS_F32) edge = fmaxf(reinterpret_cast<const float *>(at)[edge_at], LOWEST);
+            else edge = fmaxf(attn::low<DT == SAE_KV_F16>((uint32_t)reinterpret_cast<const uint16_t *>(at)[edge_at]), LOWEST);
+        }
+#pragma unroll 1
+        for (int v0 = 0; v0 < vectors; v0 += GROUPS * THREADS) {
+#pragma unroll
+            for (int g0 = 0; g0 < GROUPS; g0 += UN) {
+                if (v0 + g0 * THREADS >= vectors) break;  // uniform
+                u32x4 x[UN];
+#pragma unroll
+                for (int i = 0; i < UN; ++i) x[i] = vector(min(v0 + (g0 + i) * THREADS + (int)threadIdx.x, vectors - 1));
+#pragma unroll
+                for (int i = 0; i < UN; ++i) {
+                    float m = most[g0 + i];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) m = fmaxf(m, wide(x[i], e));
+                    most[g0 + i] = v0 + (g0 + i) * THREADS + (int)threadIdx.x < vectors ? m : most[g0 + i];
+                }
+            }
+        }
+        float m = edge;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) m = fmaxf(m, most[g]);
+        return m;
+    }
+    // What the maxima and the edge are where +inf is the largest logit.
+    __device__ __forceinline__ void set_infinite()
+    {
+        infinite = true;
+        edge = mapped(edge);
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) most[g] = mapped(most[g]);
+    }
+    // f(logit, index) for every logit.
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const
+    {
+#pragma unroll 1
+        for (int v = threadIdx.x; v < vectors; v += THREADS * UN) {
+            u32x4 x[UN];
+#pragma unroll
+            for (int k = 0; k < UN; ++k) x[k] = vector(min(v + k * THREADS, vectors - 1));
+#pragma unroll
+            for (int k = 0; k < UN; ++k)
+                if (v + k * THREADS < vectors) use(x[k], v + k * THREADS, f);
+        }
+        if (edge_at >= 0) f(edge, edge_at);
+    }
+    // f(logit, index) for every logit >= bound, and others.
+    template <typename F>
+    __device__ __forceinline__ void some(float bound, F f) const
+    {
+        uint32_t groups = 0;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) groups |= most[g] >= bound ? 1u << g : 0u;
+        while (groups) {
+            const int g = __builtin_ctz(groups);
+            groups &= groups - 1;
+#pragma unroll 1
+            for (int v = g * THREADS + (int)threadIdx.x; v < vectors; v += GROUPS * THREADS) use(vector(v), v, f);
+        }
+        if (edge >= bound && edge_at >= 0) f(edge, edge_at);
+    }
+
+private:
+    template <typename F>
+    __device__ __forceinline__ void use(u32x4 x, int v, F f) const
+    {
+        if (infinite) {  // uniform
+#pragma unroll 1
+            for (int i = 0; i < E; ++i) f(mapped(wide(x, i)), head + v * E + i);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) f(wide(x, i), head + v * E + i);
+    }
 };
 
 // A row's weights and bins.
 struct Scale {
-    float top, bins_per;  // l_0; bins of a unit of l_0 - l
-    double c;             // log2 e / T
+    double top, c;        // l_0; 32 log2 e / T
+    const double *power;
 
-    // 2^((l - l_0) c) in units of 2^-43, by the Taylor series of its fractional part (next term 6e-15).
-    __device__ __forceinline__ u64 weight(float l) const
+    // (l_0 - l) / T in 32nds of a factor of two, as a whole number and a rest in +-1/2; NaN and -inf: LIGHT
+    __device__ __forceinline__ int split(float l, double &rest) const
     {
-        if (l == top) return (u64)ONE;
-        if (top == __builtin_inff()) return 0;
-        const double z = ((double)l - (double)top) * c;
-        if (!(z > -46.0)) return 0;
-        const double n = __builtin_rint(z), f = (z - n) * 0.693147180559945309417;
-        double y = 1.0 / 39916800;
-        y = __builtin_fma(y, f, 1.0 / 3628800);
-        y = __builtin_fma(y, f, 1.0 / 362880);
-        y = __builtin_fma(y, f, 1.0 / 40320);
-        y = __builtin_fma(y, f, 1.0 / 5040);
-        y = __builtin_fma(y, f, 1.0 / 720);
-        y = __builtin_fma(y, f, 1.0 / 120);
-        y = __builtin_fma(y, f, 1.0 / 24);
-        y = __builtin_fma(y, f, 1.0 / 6);
-        y = __builtin_fma(y, f, 0.5);
-        y = __builtin_fma(y, f, 1.0);
-        y = __builtin_fma(y, f, 1.0);
-        // rounded to a whole number by 2^52, whose last bit is 1
-        const double w = __builtin_ldexp(y, (int)n + 43) + 4503599627370496.0;
-        return (u64)__double_as_longlong(w) & 0xFFFFFFFFFFFFFull;
+        const double y = __builtin_fmin((top - (double)l) * c, (double)LIGHT);
+        const double t = y + 4503599627370496.0;  // 2^52: the sum's last bits are y's whole number
+        rest = y - (t - 4503599627370496.0);
+        return (int)__double2loint(t);
     }
-    // Rises as l falls; the last one for tokens that weigh nothing (and others as light).
     __device__ __forceinline__ int bin(float l) const
     {
-        if (l == top) return 0;
-        if (top == __builtin_inff()) return BINS - 1;
-        const float x = fminf(top - l, 3.4028235e38f) * bins_per;
-        return x < (float)(BINS - 1) ? (int)x : BINS - 1;
+        double rest;
+        return split(l, rest);
     }
+    // exp((l - l_0) / T) in units of 2^-43 by the rest's Taylor series (next term 2e-15) and a table of 32 powers.
+    __device__ __forceinline__ u64 weight(int n, double rest) const
+    {
+        constexpr double A = -0.693147180559945309417 / PER_TWO;
+        double y = __builtin_fma(rest, A * A * A * A * A / 120, A * A * A * A / 24);
+        y = __builtin_fma(rest, y, A * A * A / 6);
+        y = __builtin_fma(rest, y, A * A / 2);
+        y = __builtin_fma(rest, y, A);
+        y = __builtin_fma(rest, y, 1.0);
+        // 2^(-n / 32): the table's by the last bits of n, the others are the exponent's
+        const double p = power[n & (PER_TWO - 1)];
+        const double q = __hiloint2double(__double2hiint(p) - (int)((uint32_t)n / PER_TWO << 20), __double2loint(p));
+        // rounded to a whole number by 2^52, whose last bit is 1
+        return (u64)__double_as_longlong(__builtin_fma(y, q, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+    }
+    __device__ __forceinline__ u64 weight(float l) const
+    {
+        double rest;
+        const int n = split(l, rest);
+        return weight(n, rest);
+    }
+    // A logit that those of bins 0 .. b are not below, and bins from b + 2 on are not above.
+    __device__ __forceinline__ float floor_of(int b) const { return __double2float_rd(top - (b + 1.0) / c); }
 };
 
-__device__ __forceinline__ void clear(Hist &h)
-{
-    for (int i = threadIdx.x; i < BINS; i += THREADS) {
-        h.mass[i] = 0;
-        h.count[i] = 0;
-    }
-}
-
 // Counts and masses up to each bin, itself included.
-__device__ __forceinline__ void accumulate(Shared &s, Hist &h)
+template <int NW, int N>
+__device__ __forceinline__ void accumulate(Shared &s, u64 *mass, uint32_t *count)
 {
-    static_assert(BINS == 2 * THREADS, "two bins a thread");
-    const int i = threadIdx.x * 2;
-    const uint32_t c0 = h.count[i], c1 = h.count[i + 1];
-    const u64 m0 = h.mass[i], m1 = h.mass[i + 1];
-    uint32_t ct;
-    u64 mt;
-    const uint32_t c = scan<NW>(c0 + c1, ct, s.tmp32);
-    const u64 m = scan<NW>(m0 + m1, mt, s.tmp);
-    h.count[i] = c + c0;
-    h.count[i + 1] = c + c0 + c1;
-    h.mass[i] = m + m0;
-    h.mass[i + 1] = m + m0 + m1;
+    constexpr int PER = (N + NW * SAE_WAVE - 1) / (NW * SAE_WAVE);
+    const int i0 = threadIdx.x * PER;
+    u64 m[PER];
+    uint32_t c[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        m[i] = i0 + i < N ? mass[i0 + i] : 0;
+        c[i] = i0 + i < N ? count[i0 + i] : 0;
+        if (i) {
+            m[i] += m[i - 1];
+            c[i] += c[i - 1];
+        }
+    }
+    const uint32_t cb = sum_before<NW>(s, 0, c[PER - 1]);
+    const u64 mb = sum_before<NW>(s, 1, m[PER - 1]);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (i0 + i < N) {
+            mass[i0 + i] = mb + m[i];
+            count[i0 + i] = cb + c[i];
+        }
     __syncthreads();
 }
 
-// The first bin up to which `pred(count, mass)` holds (it stays true from there on); BINS - 1 where none is.
-template <typename P>
-__device__ __forceinline__ int first_bin(Shared &s, const Hist &h, P pred)
+// The first i < n for which pred(i) holds (it holds from there on); n - 1 where none does.
+template <int THREADS, typename P>
+__device__ __forceinline__ int first_of(Shared &s, int n, P pred)
 {
     __syncthreads();
-    if (threadIdx.x == 0) s.found = BINS - 1;
+    if (threadIdx.x == 0) s.found = n - 1;
     __syncthreads();
-    for (int i = threadIdx.x; i < BINS; i += THREADS)
-        if (pred(h.count[i], h.mass[i]) && (i == 0 || !pred(h.count[i - 1], h.mass[i - 1]))) s.found = i;
+    for (int i = threadIdx.x; i < n; i += THREADS)
+        if (pred(i) && (i == 0 || !pred(i - 1))) s.found = i;
     __syncthreads();
     return uniform((int)s.found);
 }
 
 // Sorts s.list[0 .. n - 1] and fills s.sums with the weights up to each, after `before`.
+template <int NW>
 __device__ __forceinline__ void sort_and_sum(Shared &s, const Scale &sc, int n, u64 before)
 {
+    constexpr int THREADS = NW * SAE_WAVE, PER = (LIST + THREADS - 1) / THREADS;
     int size = 2;
     while (size < n) size *= 2;
     for (int i = n + threadIdx.x; i < size; i += THREADS) s.list[i] = ~0ull;
@@ -211,8 +346,8 @@ __device__ __forceinline__ void sort_and_sum(Shared &s, const Scale &sc, int n, 
     for (int k = 2; k <= size; k *= 2)
 #pragma unroll 1
         for (int j = k / 2; j > 0; j /= 2) {
-            const int i = threadIdx.x / j * 2 * j + threadIdx.x % j;
-            if (i < size) {
+            for (int t = threadIdx.x; t < size / 2; t += THREADS) {
+                const int i = (t & ~(j - 1)) * 2 + (t & (j - 1));
                 const u64 a = s.list[i], b = s.list[i + j];
                 if ((a > b) == ((i & k) == 0)) {
                     s.list[i] = b;
@@ -221,66 +356,70 @@ __device__ __forceinline__ void sort_and_sum(Shared &s, const Scale &sc, int n, 
             }
             __syncthreads();
         }
-    const int i = threadIdx.x * 2;
-    const u64 a = i < n ? sc.weight(logit_of((uint32_t)(s.list[i] >> 32))) : 0;
-    const u64 b = i + 1 < n ? sc.weight(logit_of((uint32_t)(s.list[i + 1] >> 32))) : 0;
-    u64 total;
-    const u64 m = before + scan<NW>(a + b, total, s.tmp);
-    if (i < n) s.sums[i] = m + a;
-    if (i + 1 < n) s.sums[i + 1] = m + a + b;
+    const int per = (n + THREADS - 1) / THREADS, i0 = threadIdx.x * per;
+    u64 m[PER], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (i < per && i0 + i < n) sum += sc.weight(logit_of((uint32_t)(s.list[i0 + i] >> 32)));
+        m[i] = sum;
+    }
+    const u64 mb = before + sum_before<NW>(s, 0, sum);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (i < per && i0 + i < n) s.sums[i0 + i] = mb + m[i];
     __syncthreads();
-}
-
-// The number of the list's tokens before the first one for which pred(sum up to it) holds.
-template <typename P>
-__device__ __forceinline__ int first_sum(Shared &s, int n, P pred)
-{
-    __syncthreads();
-    if (threadIdx.x == 0) s.found = n;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += THREADS)
-        if (pred(s.sums[i]) && (i == 0 || !pred(s.sums[i - 1]))) s.found = i;
-    __syncthreads();
-    return uniform((int)s.found);
 }
 
 __device__ __forceinline__ u64 uniform64(u64 x) { return (u64)uniform((long long)x); }
+__device__ __forceinline__ u64 share(float p, u64 of, bool up)
+{
+    const double x = (double)p * (double)of;
+    return (u64)(up ? __builtin_ceil(x) : __builtin_floor(x));
+}
+// A token is drawn where the sum passes this.
+__device__ __forceinline__ u64 drawn_at(float u, u64 sum) { return u > 0.0f ? min(share(fminf(u, 1.0f), sum, false), sum - 1) : 0; }
 
-// The head of the order that a question asks for, when its tokens are not in the list: the first
-// n tokens where BY_COUNT (target = n), else the shortest whose mass is at least target.
+// The head of the order that a question asks for: the first `target` tokens where by_count, else the shortest
+// whose mass is at least `target`.
 struct Head {
     u64 n, mass;
-    u64 last;         // weight of its last token
-    uint32_t index;   // of its last token (where asked for)
+    u64 last;        // weight of its last token
+    uint32_t index;  // of its last token (where asked for)
 };
 
-template <int DT>
-__device__ __forceinline__ Head locate(Shared &s, const Row<DT> &row, const Scale &sc, bool by_count, u64 target, bool index)
+template <int DT, int THREADS>
+__device__ __forceinline__ Head locate(Shared &s, const Row<DT, THREADS> &row, const Scale &sc, bool by_count, u64 target, bool index)
 {
+    constexpr int NW = THREADS / SAE_WAVE;
     auto reached = [&](u64 n, u64 mass) { return (by_count ? n : mass) >= target; };
-    const int b = first_bin(s, s.bins, [&](uint32_t n, u64 mass) { return reached(n, mass); });
+    const int b = first_of<THREADS>(s, BINS, [&](int i) { return reached(s.bins.count[i], s.bins.mass[i]); });
     u64 n0 = b ? s.bins.count[b - 1] : 0, m0 = b ? s.bins.mass[b - 1] : 0;
     uint32_t left = s.bins.count[b] - (uint32_t)n0;
-    // tokens of the bin whose keys agree with `key` above bit `shift`
+    if (by_count && b >= LIGHT) return {target, m0, 0, 0};  // (its tokens weigh nothing)
+    // tokens of the bin whose keys agree with `key` from bit `shift` on
+    const float lo = b >= LIGHT - 1 ? LOWEST : sc.floor_of(b), hi = b < 3 ? __builtin_inff() : sc.floor_of(b - 3);
     uint32_t key = 0;
     int shift = 32;
     auto inside = [&](float l) {
-        return l > attn::NEG_INF && sc.bin(l) == b && (shift == 32 || key_of(l) >> shift == key >> shift);
+        return l >= lo && l <= hi && l > LOWEST && sc.bin(l) == b && (shift == 32 || key_of(l) >> shift == key >> shift);
     };
     while (left > LIST && shift > 0) {
-        const int bits = shift == 32 ? 11 : min(shift, 11), next = shift - bits;
+        const int next = max(shift - 10, 0), mask = (1 << (shift - next)) - 1;
         __syncthreads();
-        clear(s.digits);
+        for (int i = threadIdx.x; i < DIGITS; i += THREADS) {
+            s.digits.mass[i] = 0;
+            s.digits.count[i] = 0;
+        }
         __syncthreads();
         row.each([&](float l, int) {
             if (!inside(l)) return;
-            const int d = (int)(key_of(l) >> next) & ((1 << bits) - 1);
+            const int d = (int)(key_of(l) >> next) & mask;
             atomicAdd(&s.digits.count[d], 1u);
             atomicAdd(&s.digits.mass[d], sc.weight(l));
         });
         __syncthreads();
-        accumulate(s, s.digits);
-        const int d = first_bin(s, s.digits, [&](uint32_t n, u64 mass) { return reached(n0 + n, m0 + mass); });
+        accumulate<NW, DIGITS>(s, s.digits.mass, s.digits.count);
+        const int d = first_of<THREADS>(s, DIGITS, [&](int i) { return reached(n0 + s.digits.count[i], m0 + s.digits.mass[i]); });
         const uint32_t before = d ? s.digits.count[d - 1] : 0;
         left = s.digits.count[d] - before;
         m0 += d ? s.digits.mass[d - 1] : 0;
@@ -297,8 +436,8 @@ __device__ __forceinline__ Head locate(Shared &s, const Row<DT> &row, const Scal
         });
         __syncthreads();
         const int n = uniform((int)s.n);
-        sort_and_sum(s, sc, n, m0);
-        const int at = by_count ? min((int)(target - n0), n) - 1 : min(first_sum(s, n, [&](u64 sum) { return sum >= target; }), n - 1);
+        sort_and_sum<NW>(s, sc, n, m0);
+        const int at = by_count ? min((int)(target - n0), n) - 1 : first_of<THREADS>(s, n, [&](int i) { return s.sums[i] >= target; });
         const u64 sum = uniform64(s.sums[at]);
         return {n0 + at + 1, sum, sum - (at ? uniform64(s.sums[at - 1]) : m0), (uint32_t)uniform64(s.list[at])};
     }
@@ -310,14 +449,17 @@ __device__ __forceinline__ Head locate(Shared &s, const Row<DT> &row, const Scal
     uint32_t at = 0, before = 0;
     for (int next = 10; next >= 0; next -= 10) {
         __syncthreads();
-        clear(s.digits);
+        for (int i = threadIdx.x; i < DIGITS; i += THREADS) {
+            s.digits.mass[i] = 0;
+            s.digits.count[i] = 0;
+        }
         __syncthreads();
         row.each([&](float l, int i) {
             if (inside(l) && (next == 10 || (uint32_t)i >> 10 == at >> 10)) atomicAdd(&s.digits.count[i >> next & 1023], 1u);
         });
         __syncthreads();
-        accumulate(s, s.digits);
-        const int d = first_bin(s, s.digits, [&](uint32_t n, u64) { return before + n >= r; });
+        accumulate<NW, DIGITS>(s, s.digits.mass, s.digits.count);
+        const int d = first_of<THREADS>(s, DIGITS, [&](int i) { return before + s.digits.count[i] >= r; });
         before += d ? s.digits.count[d - 1] : 0;
         at |= (uint32_t)d << next;
     }
@@ -325,63 +467,57 @@ __device__ __forceinline__ Head locate(Shared &s, const Row<DT> &row, const Scal
     return h;
 }
 
-__device__ __forceinline__ u64 share(float p, u64 of, bool up)
-{
-    const double x = (double)p * (double)of;
-    return (u64)(up ? __builtin_ceil(x) : __builtin_floor(x));
-}
-
-template <int DT>
+template <int DT, int THREADS>
 __global__ void __launch_bounds__(THREADS) k_sample(Args a)
 {
+    constexpr int NW = THREADS / SAE_WAVE;
     __shared__ Shared s;
     const int r = blockIdx.x, lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
-    const Row<DT> row(static_cast<const char *>(a.logits) + (int64_t)r * a.stride * Row<DT>::SIZE, a.vocab);
+    Row<DT, THREADS> row(static_cast<const char *>(a.logits) + (int64_t)r * a.stride * Row<DT, THREADS>::SIZE, a.vocab);
     const float T = a.temperature ? a.temperature[r] : 1.0f, p = a.top_p ? a.top_p[r] : 1.0f, m = a.min_p ? a.min_p[r] : 0.0f;
     const int k = a.top_k ? a.top_k[r] : 0;
     const float u = a.u[r];
     auto answer = [&](uint32_t token, float prob, uint32_t kept) {
-        if (threadIdx.x) return;
         a.token[r] = (int32_t)token;
         if (a.prob) a.prob[r] = prob;
         if (a.kept) a.kept[r] = (int32_t)kept;
     };
+    if (threadIdx.x < PER_TWO) s.power[threadIdx.x] = __builtin_ldexp(exp2(threadIdx.x * (-1.0 / PER_TWO)), 43);
 
-    float mine = attn::NEG_INF;
-    row.each([&](float l, int) { mine = fmaxf(mine, l); });
-    float top = over_wave(mine, [](float x, float y) { return fmaxf(x, y); });
-    if (lane == 0) s.tmp32[wave] = __float_as_uint(top);
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, __uint_as_float(s.tmp32[w]));
-    __syncthreads();
-    if (!(top > attn::NEG_INF)) return answer(~0u, 0.0f, 0);
+    float mine = row.maxima();
+    float top = over_all<NW>(s, 0, mine, LOWEST, [](float x, float y) { return fmaxf(x, y); });
+    if (!(top > LOWEST)) {
+        if (threadIdx.x == 0) answer(~0u, 0.0f, 0);
+        return;
+    }
+    if (top == __builtin_inff()) {  // uniform
+        row.set_infinite();
+        mine = row.mapped(mine);
+        top = 0.0f;
+    }
     if (!(T > 0.0f) || k == 1 || p <= 0.0f) {  // the first of the largest
         uint32_t first = ~0u;
-        row.each([&](float l, int i) {
+        row.some(top, [&](float l, int i) {
             if (l == top) first = min(first, (uint32_t)i);
         });
-        first = over_wave(first, [](uint32_t x, uint32_t y) { return min(x, y); });
-        if (lane == 0) s.tmp32[wave] = first;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < NW; ++w) first = min(first, s.tmp32[w]);
-        return answer(first, 1.0f, 1);
+        first = over_all<NW>(s, 1, first, ~0u, [](uint32_t x, uint32_t y) { return min(x, y); });
+        if (threadIdx.x == 0) answer(first, 1.0f, 1);
+        return;
     }
-    const Scale sc = {top, PER_UNIT / T, 1.44269504088896340736 / (double)T};
+    const Scale sc = {(double)top, PER_TWO * 1.44269504088896340736 / (double)T, s.power};
 
     // the list: the first tokens of the order, enough of them for every question
-    int n = LIST + 1;       // in the list; more than LIST: not collected
-    bool whole = false;     // the list holds every token, or `total` is the weight of all
+    int n = LIST + 1;    // in the list; more than LIST: not collected
+    bool whole = false;  // `total` is the weight of all tokens, and top-k leaves them all
     u64 total = 0;
-    if (k > 0 && k <= SMALL_K) {
+    if (k > 0 && k <= THREADS / 4) {
         // the k-th largest of the threads' maxima, to 16 bits of its key
-        uint32_t bound = 0;
-        uint32_t want = (uint32_t)k;
+        uint32_t bound = 0, want = (uint32_t)k;
         const uint32_t key = key_of(mine);
 #pragma unroll 1
         for (int shift = 24; shift >= 16; shift -= 8) {
             for (int i = threadIdx.x; i < 256; i += THREADS) s.digits.count[i] = 0;
+            if (threadIdx.x == 0) s.n = 0;
             __syncthreads();
             if (shift == 24 || key >> 24 == bound >> 24) atomicAdd(&s.digits.count[key >> shift & 255], 1u);
             __syncthreads();
@@ -392,35 +528,25 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
                     c[i] = s.digits.count[lane * 4 + i];
                     sum += c[i];
                 }
-                uint32_t upto = sum;
-#pragma unroll
-                for (int o = 1; o < SAE_WAVE; o <<= 1) {
-                    const uint32_t x = __shfl_up(upto, o);
-                    if (lane >= o) upto += x;
-                }
-                uint32_t before = upto - sum;
+                uint32_t before = sum_upto(sum) - sum;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (before < want && before + c[i] >= want) {
                         s.found = lane * 4 + i;
-                        s.n = want - before;
+                        s.want = want - before;
                     }
                     before += c[i];
                 }
             }
             __syncthreads();
             bound |= s.found << shift;
-            want = s.n;
-            __syncthreads();
+            want = s.want;
         }
-        bound |= 0xFFFFu;  // keys up to it
-        if (threadIdx.x == 0) s.n = 0;
-        __syncthreads();
-        row.each([&](float l, int i) {
-            const uint32_t x = key_of(l);
-            if (l > attn::NEG_INF && x <= bound) {
+        const float least = fmaxf(logit_of(bound | 0xFFFFu), -0x1.fffffep127f);  // (-inf is not taken)
+        row.some(least, [&](float l, int i) {
+            if (l >= least) {
                 const uint32_t at = atomicAdd(&s.n, 1u);
-                if (at < LIST) s.list[at] = (u64)x << 32 | (uint32_t)i;
+                if (at < LIST) s.list[at] = (u64)key_of(l) << 32 | (uint32_t)i;
             }
         });
         __syncthreads();
@@ -428,70 +554,93 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
     }
     u64 kth = 0;  // tokens that top-k leaves
     if (n > LIST) {
-        clear(s.bins);
         __syncthreads();
-        uint32_t light = 0;  // tokens of the last bin
+        for (int i = threadIdx.x; i < BINS; i += THREADS) {
+            s.bins.mass[i] = 0;
+            s.bins.count[i] = 0;
+        }
+        if (threadIdx.x == 0) s.n = 0;
+        __syncthreads();
+        uint32_t light = 0;
         row.each([&](float l, int) {
-            if (!(l > attn::NEG_INF)) return;
-            const int b = sc.bin(l);
-            if (b == BINS - 1) {
-                ++light;
-                return;
+            double rest;
+            const int b = sc.split(l, rest);
+            if (b < LIGHT) {
+                atomicAdd(&s.bins.count[b], 1u);
+                atomicAdd(&s.bins.mass[b], sc.weight(b, rest));
+            } else {
+                light += l > LOWEST;
             }
-            atomicAdd(&s.bins.count[b], 1u);
-            atomicAdd(&s.bins.mass[b], sc.weight(l));
         });
-        light = over_wave(light, [](uint32_t x, uint32_t y) { return x + y; });
-        if (lane == 0 && light) atomicAdd(&s.bins.count[BINS - 1], light);
+        light = sum_upto(light);
+        if (lane == SAE_WAVE - 1 && light) atomicAdd(&s.bins.count[LIGHT], light);
         __syncthreads();
-        accumulate(s, s.bins);
+        accumulate<NW, BINS>(s, s.bins.mass, s.bins.count);
         const uint32_t all = s.bins.count[BINS - 1];
         total = s.bins.mass[BINS - 1];
         kth = k > 0 && (uint32_t)k < all ? (uint32_t)k : all;
-        int last = first_bin(s, s.bins, [&](uint32_t c, u64) { return c >= kth; });
         whole = kth == all;
+        int last = whole ? LIGHT : first_of<THREADS>(s, BINS, [&](int i) { return s.bins.count[i] >= kth; });
         // (top-p of what top-k leaves: its weight has to be known first)
-        if (p < 1.0f && whole) {
+        if (whole && p < 1.0f) {
             const u64 most = share(p, total, true);
-            last = min(last, first_bin(s, s.bins, [&](uint32_t, u64 mass) { return mass >= most; }));
+            last = first_of<THREADS>(s, BINS, [&](int i) { return s.bins.mass[i] >= most; });
         }
         if (m > 0.0f && (whole || !(p < 1.0f))) {
-            const float x = -__builtin_logf(fminf(m, 1.0f)) * PER_UNIT + 2.0f;
+            const float x = -log2f(fminf(m, 1.0f)) * PER_TWO + 2.0f;
             if (x < (float)last) last = (int)x;
         }
         n = (int)s.bins.count[last];
         if (n <= LIST) {
-            if (threadIdx.x == 0) s.n = 0;
-            __syncthreads();
-            row.each([&](float l, int i) {
-                if (l > attn::NEG_INF && sc.bin(l) <= last) s.list[min(atomicAdd(&s.n, 1u), (uint32_t)LIST - 1)] = (u64)key_of(l) << 32 | (uint32_t)i;
+            const float least = last >= LIGHT - 1 ? -0x1.fffffep127f : sc.floor_of(last);
+            row.some(least, [&](float l, int i) {
+                if (l >= least && sc.bin(l) <= last) s.list[min(atomicAdd(&s.n, 1u), (uint32_t)LIST - 1)] = (u64)key_of(l) << 32 | (uint32_t)i;
             });
             __syncthreads();
         }
     }
-    if (n <= LIST) {
-        sort_and_sum(s, sc, n, 0);
+    if (n <= SAE_WAVE) {  // one wave, a token a lane
+        if (wave != 0) return;
+        u64 item = lane < n ? s.list[lane] : ~0ull;
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += of_lane(item, j) < item;
+        if (lane < n) s.list[rank] = item;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        item = s.list[lane];
+        const u64 w = lane < n ? sc.weight(logit_of((uint32_t)(item >> 32))) : 0, sum = sum_upto(w);
         int keep = k > 0 ? min(k, n) : n;
-        const u64 of = whole ? total : uniform64(s.sums[keep - 1]);
+        auto first = [&](bool x) { return __builtin_ctzll(__ballot(x) | 1ull << (keep - 1)); };
         if (p < 1.0f) {
-            const u64 target = share(p, of, true);
-            keep = min(keep, first_sum(s, n, [&](u64 sum) { return sum >= target; }) + 1);
+            const u64 target = share(p, whole ? total : of_lane(sum, keep - 1), true);
+            keep = first(sum >= target) + 1;
         }
         if (m > 0.0f) {
             const double least = (double)m * ONE;
-            __syncthreads();
-            if (threadIdx.x == 0) s.found = keep;
-            __syncthreads();
-            for (int i = threadIdx.x; i < keep; i += THREADS)
-                if ((double)(s.sums[i] - (i ? s.sums[i - 1] : 0)) < least) atomicMin(&s.found, (uint32_t)i);
-            __syncthreads();
-            keep = max(1, uniform((int)s.found));
+            const u64 light = __ballot(lane < n && (double)w < least);
+            if (light) keep = max(min(keep, __builtin_ctzll(light)), 1);
         }
-        const u64 sum = uniform64(s.sums[keep - 1]);
-        const u64 target = u > 0.0f ? min(share(fminf(u, 1.0f), sum, false), sum - 1) : 0;
-        const int at = first_sum(s, keep, [&](u64 x) { return x > target; });
-        const u64 w = s.sums[at] - (at ? s.sums[at - 1] : 0);
-        return answer((uint32_t)s.list[at], (float)((double)w / (double)sum), keep);
+        const u64 of = of_lane(sum, keep - 1), target = drawn_at(u, of);
+        const int at = first(sum > target);
+        if (lane == at) answer((uint32_t)item, (float)((double)w / (double)of), keep);
+        return;
+    }
+    if (n <= LIST) {
+        sort_and_sum<NW>(s, sc, n, 0);
+        int keep = k > 0 ? min(k, n) : n;
+        if (p < 1.0f) {
+            const u64 target = share(p, whole ? total : uniform64(s.sums[keep - 1]), true);
+            keep = first_of<THREADS>(s, keep, [&](int i) { return s.sums[i] >= target; }) + 1;
+        }
+        if (m > 0.0f) {
+            const double least = (double)m * ONE;
+            auto light = [&](int i) { return (double)(s.sums[i] - (i ? s.sums[i - 1] : 0)) < least; };
+            const int at = first_of<THREADS>(s, keep, light);
+            if (light(at)) keep = max(at, 1);
+        }
+        const u64 of = uniform64(s.sums[keep - 1]), target = drawn_at(u, of);
+        const int at = first_of<THREADS>(s, keep, [&](int i) { return s.sums[i] > target; });
+        if (threadIdx.x == 0) answer((uint32_t)s.list[at], (float)((double)(s.sums[at] - (at ? s.sums[at - 1] : 0)) / (double)of), keep);
+        return;
     }
     // too many for the list: each question by itself
     Head h = {kth, total, 0, 0};
@@ -499,10 +648,12 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
     for (int question = 0;; ++question) {  // top-k, top-p, min-p, the token
         if ((question == 0 && whole) || (question == 1 && !(p < 1.0f)) || (question == 2 && !(m > 0.0f))) continue;
         if (question != 2) {
-            const u64 target = question == 0 ? kth : question == 1 ? max(share(p, h.mass, true), 1ull)
-                               : u > 0.0f ? min(share(fminf(u, 1.0f), h.mass, false), h.mass - 1) + 1 : 1;
+            const u64 target = question == 0 ? kth : question == 1 ? max(share(p, h.mass, true), 1ull) : drawn_at(u, h.mass) + 1;
             const Head found = locate(s, row, sc, question == 0, target, question == 3);
-            if (question == 3) return answer(found.index, (float)((double)found.last / (double)h.mass), (uint32_t)h.n);
+            if (question == 3) {
+                if (threadIdx.x == 0) answer(found.index, (float)((double)found.last / (double)h.mass), (uint32_t)h.n);
+                return;
+            }
             h = found;
             continue;
         }
@@ -510,23 +661,25 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
         uint32_t c = 0;
         u64 mass = 0;
         row.each([&](float l, int) {
-            if (!(l > attn::NEG_INF)) return;
             const u64 w = sc.weight(l);
-            if ((double)w >= least) {
-                ++c;
-                mass += w;
-            }
+            const bool in = (double)w >= least && l > LOWEST;
+            c += in;
+            mass += in ? w : 0;
         });
-        u64 c_all, m_all;
-        scan<NW>((u64)c, c_all, s.tmp);
         __syncthreads();
-        scan<NW>(mass, m_all, s.tmp);
-        if (c_all == 0) {
-            c_all = 1;
-            m_all = (u64)ONE;
-        }
-        if (c_all < h.n) h = {c_all, m_all, 0, 0};
+        const uint32_t c_all = over_all<NW>(s, 0, c, 0u, [](uint32_t x, uint32_t y) { return x + y; });
+        const u64 m_all = over_all<NW>(s, 1, mass, (u64)0, [](u64 x, u64 y) { return x + y; });
+        if (c_all == 0) h = {1, (u64)ONE, 0, 0};  // (min-p above 1)
+        else if (c_all < h.n) h = {c_all, m_all, 0, 0};
     }
+}
+
+template <int DT>
+void launch(const Args &a, int rows, hipStream_t s)
+{
+    if (a.vocab <= 8192) hipLaunchKernelGGL((k_sample<DT, 256>), dim3(rows), dim3(256), 0, s, a);
+    else if (rows >= 512) hipLaunchKernelGGL((k_sample<DT, 512>), dim3(rows), dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_sample<DT, 1024>), dim3(rows), dim3(1024), 0, s, a);
 }
 
 }  // namespace
@@ -537,8 +690,8 @@ hipError_t launch_sample(int rows, int vocab, int dtype, const SampleArgs &x, hi
 {
     const Args a = {x.logits, x.stride, x.settings.temperature, x.settings.top_p, x.settings.min_p, x.u, x.settings.top_k,
                     x.token, x.kept, x.prob, vocab};
-    if (dtype == SAE_KV_BF16) hipLaunchKernelGGL((k_sample<SAE_KV_BF16>), dim3(rows), dim3(THREADS), 0, s, a);
-    else if (dtype == SAE_KV_F16) hipLaunchKernelGGL((k_sample<SAE_KV_F16>), dim3(rows), dim3(THREADS), 0, s, a);
-    else hipLaunchKernelGGL((k_sample<SAE_ROWS_F32>), dim3(rows), dim3(THREADS), 0, s, a);
+    if (dtype == SAE_KV_BF16) launch<SAE_KV_BF16>(a, rows, s);
+    else if (dtype == SAE_KV_F16) launch<SAE_KV_F16>(a, rows, s);
+    else launch<SAE_ROWS_F32>(a, rows, s);
     return hipGetLastError();
 }

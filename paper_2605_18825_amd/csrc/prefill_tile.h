@@ -93,6 +93,7 @@ struct Plan {
     int groups;  // workgroups per key-value head that fill the GPU, over which long tiles'
                  // keys are split; 0: none is
     int most;    // parts of a tile at most (from the keys that the table holds)
+    int slots;   // parts that the workspace holds
 };
 
 // The rows of a workgroup and the keys they see.
@@ -158,14 +159,19 @@ __device__ __forceinline__ Tile find_tile(const KvDev &c, const AttnArgs &a, int
 struct Part {
     int seq, part, parts;  // seq < 0: none
     int sub;
+    int slot;  // the part's place in the workspace, -1 for none
+    int clear; // a place there that no part has, for this workgroup to say so; -1 for none
 };
 constexpr int PER_THREAD = 2;  // sequences of a thread at most: no more than tiles, which are 512 at most
 
-template <int NW>
+// A tree's call may have many more tiles than workgroups are wanted: parts are numbered in the
+// workspace among those of split tiles alone.  (Such a tile's keys are 3/2 shares at least and its parts at
+// most 4/3 as many as shares: 4/3 groups in all, of the 2 groups that there are.)
+template <int NW, bool TREE>
 __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, const Plan &plan, int x, int rows, int keys)
 {
-    __shared__ long long tmp[2][NW], found_rest;
-    __shared__ int found_seq, found_parts;
+    __shared__ long long tmp[TREE ? 3 : 2][NW], found_rest;
+    __shared__ int found_seq, found_parts, found_slot;
     const int G = a.heads / c.kvh, chunk = (c.n_seq + NW * SAE_WAVE - 1) / (NW * SAE_WAVE);
     // tiles of sequence r, and the mean of their steps, about
     auto size = [&](int r, int &tiles, int &steps) {
@@ -178,11 +184,14 @@ __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, con
     auto share_of = [&](long long total) {
         return (int)max((total + plan.groups - 1) / plan.groups, (long long)(MIN_SPLIT / keys));
     };
+    auto parts_of_share = [&](int steps, int share) { return min(max((steps + (TREE ? share / 2 : 0)) / share, 1), plan.most); };
     if (c.n_seq == 1) {  // uniform: no scans
         int tiles, steps;
         size(0, tiles, steps);
-        const int parts = min(max(steps / share_of((long long)tiles * steps), 1), plan.most);
-        return {x < (long long)tiles * parts ? 0 : -1, x % parts, parts, x / parts};
+        const int parts = parts_of_share(steps, share_of((long long)tiles * steps));
+        const bool there = x < (long long)tiles * parts;
+        const bool held = there && parts > 1;
+        return {there ? 0 : -1, x % parts, parts, x / parts, TREE && !held ? -1 : x, TREE && !held ? x : -1};
     }
     const int r0 = min((int)threadIdx.x * chunk, c.n_seq);
     int tiles[PER_THREAD], steps[PER_THREAD];
@@ -198,13 +207,15 @@ __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, con
     long long total;
     scan<NW>(work, total, tmp[0]);
     const int share = share_of(total);
-    long long count = 0;
+    long long count = 0, held = 0, all_held = 0, held_before = 0;
 #pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
-        steps[i] = min(max(steps[i] / share, 1), plan.most);  // parts from here on
+        steps[i] = parts_of_share(steps[i], share);  // parts from here on
         count += (long long)tiles[i] * steps[i];
+        if (TREE && steps[i] > 1) held += (long long)tiles[i] * steps[i];
     }
     long long before = scan<NW>(count, total, tmp[1]);
+    if constexpr (TREE) held_before = scan<NW>(held, all_held, tmp[2]);
     if (x >= before && x < before + count) {  // one thread
 #pragma unroll
         for (int i = 0; i < PER_THREAD; ++i) {
@@ -213,14 +224,17 @@ __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, con
                 found_seq = r0 + i;
                 found_parts = steps[i];
                 found_rest = x - before;
+                if (TREE) found_slot = steps[i] > 1 ? (int)(held_before + x - before) : -1;
             }
             before += k;
+            if (TREE && steps[i] > 1) held_before += k;
         }
     }
     __syncthreads();
-    if (x >= total) return {-1, 0, 1, 0};
+    const int clear = TREE && x >= all_held ? x : -1;
+    if (x >= total) return {-1, 0, 1, 0, -1, clear};
     const int parts = uniform(found_parts), rest = uniform((int)found_rest);
-    return {uniform(found_seq), rest % parts, parts, rest / parts};
+    return {uniform(found_seq), rest % parts, parts, rest / parts, TREE ? uniform(found_slot) : x, clear};
 }
 
 // A split tile as the workspace has it, by the workgroup of its first part.
@@ -406,7 +420,7 @@ __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, const Mas
 // workgroup, head and wave a part's outputs, maxima and sums as the lanes hold them.
 __device__ __forceinline__ float *parts_of(const AttnArgs &a, const Plan &plan)
 {
-    return reinterpret_cast<float *>(static_cast<Split *>(a.work) + (plan.groups + plan.tiles));
+    return reinterpret_cast<float *>(static_cast<Split *>(a.work) + plan.slots);
 }
 __host__ __device__ constexpr int64_t part_floats(int dim) { return ROWS * (dim + 4); }
 template <int D, int NW>
@@ -486,6 +500,7 @@ __device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const 
             a.lse[(int64_t)(t.first + token) * a.heads + head] = l == 0.0f ? NEG_INF : (m + log2_(l)) * LN2;
         return;
     }
+    if (TREE && (x >= plan.slots || wave * ROWS >= t.rows)) return;  // uniform
     // a part: maxima, sums and outputs as the lanes hold them
     float *to = parts_of(a, plan) + part_at<D, NW>(c, x, kvhead, wave);
 #pragma unroll
@@ -523,11 +538,21 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     // that the tiles that read the same keys tend to share an L2
     const int x = blockIdx.x / c.kvh, kvhead = blockIdx.x % c.kvh, G = a.heads / c.kvh;
     Tile t;
-    int part = 0, nparts = 1;
+    int part = 0, nparts = 1, slot = x;
     if constexpr (SPLIT) {
-        const Part p = find_part<NW>(c, a, plan, x, NW * ROWS, KEYS);
+        const Part p = find_part<NW, TREE>(c, a, plan, x, NW * ROWS, KEYS);
         if (p.seq >= 0) t = tile_of<TREE>(c, a, p.seq, p.sub, NW * ROWS, KEYS);
-        if (kvhead == 0 && threadIdx.x == 0)
+        slot = p.slot;
+        if constexpr (TREE) {
+            if (kvhead == 0 && threadIdx.x == 0) {
+                // (not with a q_start that decreases; no place is written past the last)
+                if (p.clear >= 0 && p.clear < plan.slots) static_cast<Split *>(a.work)[p.clear] = Split{0, 0, 0, 0};
+                if (p.slot >= 0 && p.slot < plan.slots)
+                    static_cast<Split *>(a.work)[p.slot] = p.part == 0 && p.slot + p.parts <= plan.slots
+                                                               ? Split{t.first + t.token0, t.head0, t.rows, p.parts}
+                                                               : Split{0, 0, 0, 0};
+            }
+        } else if (kvhead == 0 && threadIdx.x == 0)
             // (parts past the grid: only with a q_start that decreases)
             static_cast<Split *>(a.work)[x] = p.seq >= 0 && p.part == 0 && x + p.parts <= plan.groups + plan.tiles
                                                   ? Split{t.first + t.token0, t.head0, t.rows, p.parts}
@@ -807,7 +832,45 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
                 o[b] = mfma32<F16>(*reinterpret_cast<const u32x4 *>(vp + p * PB + b * 1024), w[p], o[b]);
     };
 
-    if (s0 < s1) {
+    if (TREE && s0 < s1 && wrow >= t.rows) {  // uniform: a wave without rows moves its share of keys and values
+        St sk, sv;
+        check_ids();
+        uint32_t holes0 = holes_of(s0);
+        const int next = min(s0 + 1, s1 - 1);
+        {
+            St k0;
+            load_k(s0, k0, k_even);
+            load_v(s0, sv, v_even);
+            load_k(next, sk, k_odd);
+            store_k(k0, k_even);
+            store_v(sv, v_even);
+            store_k(sk, k_odd);
+        }
+        uint32_t holes = holes_of(next);
+        if (a.window > 0 || s1 * KEYS > tree0) fill_masks<NW>(c, a, t, parent, *masks);
+        barrier();
+        barrier();
+        int step = s0;
+        auto body = [&](int buf) __attribute__((always_inline)) {
+            clean_v(step, holes0, lds_v[buf]);
+            const int ahead = min(step + 2, s1 - 1);
+            if (ahead >= ids_from + SAE_WAVE / PAGES) fetch_ids(step + 1);
+            holes0 = holes;
+            holes = holes_of(ahead);
+            load_k(ahead, sk, lds_k[buf]);
+            load_v(step + 1, sv, lds_v[buf ^ 1]);
+            store_k(sk, lds_k[buf]);
+            store_v(sv, lds_v[buf ^ 1]);
+            barrier();
+            ++step;
+        };
+        while (step + 1 < s1) {
+            body(0);
+            if (step + 1 >= s1) break;
+            body(1);
+        }
+        clean_v(step, holes0, (step - s0) & 1 ? v_odd : v_even);
+    } else if (s0 < s1) {
         // Step t's weights are computed while the matrix units take step t + 1's
         // scores, and that step's maximum while they add step t to the outputs: keys
         // are staged one step ahead of values.
@@ -956,7 +1019,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         outputs(w, last);
     }
 
-    finish<TYPE, D, NW, TREE>(c, a, plan, t, masks, base, kvhead, wave, x, nparts == 1, s0, s1, o, m, l);
+    finish<TYPE, D, NW, TREE>(c, a, plan, t, masks, base, kvhead, wave, slot, nparts == 1, s0, s1, o, m, l);
 }
 
 // Adds a tile's parts, in order: lanes hold what they held in k_prefill, a wave
@@ -1026,13 +1089,16 @@ int64_t tiles_of(const KvDev &c, int heads)
 // same keys spread evenly 162.
 Plan plan_of(const KvDev &c, int heads, int dim, int window, int nodes)
 {
-    Plan p = {(int)tiles_of(c, heads), 0, 1};
+    Plan p = {(int)tiles_of(c, heads), 0, 1, 0};
     // no tile has more parts than MIN_SPLIT goes into the keys that it can see
     int64_t keys = (int64_t)c.max_blocks * SAE_KV_BLOCK;
     if (window > 0) keys = std::min(keys, (int64_t)window + WAVES * ROWS + nodes + keys_of(dim));
     p.most = (int)std::min((keys + keys_of(dim)) / MIN_SPLIT, (int64_t)groups_of(dim));
-    if ((int64_t)p.tiles * c.kvh <= groups_of(dim) && c.n_seq <= PER_THREAD * WAVES * SAE_WAVE && keys > SHORT)
+    const bool few = (int64_t)p.tiles * c.kvh <= groups_of(dim);
+    if ((few || nodes > 0) && c.n_seq <= PER_THREAD * WAVES * SAE_WAVE && keys > SHORT) {
         p.groups = std::max(groups_of(dim) / c.kvh, 1);
+        p.slots = few ? p.groups + p.tiles : 2 * p.groups;
+    }
     return p;
 }
 
@@ -1045,11 +1111,11 @@ hipError_t launch(const KvDev &c, const AttnArgs &a, hipStream_t s)
         return hipGetLastError();
     }
     // parts: at most a share of the work each, rounded up for every tile
-    const unsigned grid = (unsigned)((p.groups + p.tiles) * c.kvh);
+    const unsigned grid = (unsigned)((p.groups + p.tiles) * c.kvh), joins = (unsigned)(p.slots * c.kvh);
     hipLaunchKernelGGL((k_prefill<TYPE, D, WAVES, true, TREE>), dim3(grid), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_prefill_join<TYPE, D, WAVES>), dim3(grid, D / 32), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
+    hipLaunchKernelGGL((k_prefill_join<TYPE, D, WAVES>), dim3(joins, D / 32), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
     return hipGetLastError();
 }
 
