@@ -13,6 +13,8 @@
 //   otherwise   a second pass adds every token to a histogram over (l_0 - l) / T, 32 bins for a
 //               factor of two: each bin's tokens and their weight.  The answers' bin follows, and
 //               the tokens up to it are collected.
+//   where these are many, only the tokens of the bins that the answers can lie in are: a bin is
+//   2.2 % of weight wide, and what it leaves open of one answer leaves the next one a bin or two.
 //   where these are more than LDS holds, each question is answered by itself: its bin, then
 //   (a bin of many equal or near logits) 10 bits of the logit at a time, then the index.
 #include "attn_tile.h"
@@ -93,6 +95,7 @@ struct Shared {
     u64 list[LIST];  // key << 32 | index
     double power[PER_TWO];  // 2^(-j / 32) units
     u64 part[2][16];
+    float edges[8];
     uint32_t n, found, want;
 };
 
@@ -208,6 +211,12 @@ struct Row {
     template <typename F>
     __device__ __forceinline__ void each(F f) const
     {
+        each(LOWEST, f, [](float) {});
+    }
+    // f(logit, index) for every logit; low(logit) for those of vectors that lie below `bound` whole.
+    template <typename F, typename L>
+    __device__ __forceinline__ void each(float bound, F f, L low) const
+    {
 #pragma unroll 1
         for (int v = threadIdx.x; v < vectors; v += THREADS * UN) {
             u32x4 x[UN];
@@ -215,9 +224,74 @@ struct Row {
             for (int k = 0; k < UN; ++k) x[k] = vector(min(v + k * THREADS, vectors - 1));
 #pragma unroll
             for (int k = 0; k < UN; ++k)
-                if (v + k * THREADS < vectors) use(x[k], v + k * THREADS, f);
+                if (v + k * THREADS < vectors) {
+                    if (bound > LOWEST && !infinite) {  // uniform
+                        float m = wide(x[k], 0);
+#pragma unroll
+                        for (int i = 1; i < E; ++i) m = fmaxf(m, wide(x[k], i));
+                        if (!(m >= bound)) {
+#pragma unroll
+                            for (int i = 0; i < E; ++i) low(wide(x[k], i));
+                            continue;
+                        }
+                    }
+                    use(x[k], v + k * THREADS, f);
+                }
         }
         if (edge_at >= 0) f(edge, edge_at);
+    }
+    // Appends the indexes of all logits with pred(logit) to `list`, at most `room`; n: counts them (all).
+    // Bits for four vectors at a time: a test has no branch, and a thread with any takes one place for all of them.
+    template <typename P>
+    __device__ __forceinline__ void collect(uint32_t *list, uint32_t *n, int room, P pred) const
+    {
+        auto put = [&](uint32_t at, int i) {
+            if (at < (uint32_t)room) list[at] = (uint32_t)i;
+        };
+        if (infinite) {  // uniform
+            each([&](float l, int i) {
+                if (pred(l)) put(atomicAdd(n, 1u), i);
+            });
+            return;
+        }
+#pragma unroll 1
+        for (int v = threadIdx.x; v < vectors; v += THREADS * UN) {
+            u32x4 x[UN];
+#pragma unroll
+            for (int k = 0; k < UN; ++k) x[k] = vector(min(v + k * THREADS, vectors - 1));
+            uint32_t bits = 0;
+#pragma unroll
+            for (int k = 0; k < UN; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    bits |= pred(wide(x[k], i)) ? 1u << (k * E + i) : 0u;
+                }
+            const int there = min((vectors - v + THREADS - 1) / THREADS, UN) * E;  // bits of vectors that there are
+            bits &= (uint32_t)((1ull << there) - 1);
+            if (!bits) continue;
+            uint32_t at = atomicAdd(n, (uint32_t)__builtin_popcount(bits));
+            while (bits) {
+                const int b = __builtin_ctz(bits);
+                bits &= bits - 1;
+                put(at++, head + (v + b / E * THREADS) * E + b % E);
+            }
+        }
+        if (edge_at >= 0 && pred(edge)) put(atomicAdd(n, 1u), edge_at);
+    }
+    // The logit at an index.
+    __device__ __forceinline__ float logit(int i) const
+    {
+        if constexpr (DT == SAE_ROWS_F32) return mapped(reinterpret_cast<const float *>(at)[i]);
+        else return mapped(attn::low<DT == SAE_KV_F16>((uint32_t)reinterpret_cast<const uint16_t *>(at)[i]));
+    }
+    // The bound where a whole wave's vectors of some group lie below it, else -inf: with a few below it among
+    // others a wave goes both ways.
+    __device__ __forceinline__ float any_below(float bound) const
+    {
+        bool found = false;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) found |= __all(most[g] < bound) && g * THREADS < vectors;
+        return found ? bound : LOWEST;
     }
     // f(logit, index) for every logit >= bound, and others.
     template <typename F>
@@ -292,6 +366,31 @@ struct Scale {
     __device__ __forceinline__ float floor_of(int b) const { return __double2float_rd(top - (b + 1.0) / c); }
 };
 
+// The lowest logit of bins 0 .. b (b < LIGHT), by a wave: bins do not fall as keys rise.
+__device__ __forceinline__ float lowest_of(const Scale &sc, int b)
+{
+    constexpr uint32_t FIRST = 0x00800000u, LAST = 0xFF7FFFFFu;  // keys of the largest and the lowest float
+    auto inside = [&](uint32_t k) {
+        const float l = logit_of(k);
+        return (double)l >= sc.top || sc.bin(l) <= b;
+    };
+    {  // most often within a few floats of where the bin ends
+        const uint32_t k = key_of((float)(sc.top - (b + 0.5) / sc.c)), from = k > FIRST + 32 && k < LAST - 64 ? k - 32 : FIRST;
+        const u64 in = __ballot(inside(from + (uint32_t)__lane_id()));
+        const int last = __builtin_popcountll(in) - 1;
+        if (last >= 0 && last < SAE_WAVE - 1) return logit_of(from + last);
+    }
+    uint32_t lo = FIRST, n = LAST - FIRST + 1;  // the last key with a bin up to b lies in [lo, lo + n)
+    while (n > 1) {
+        const uint32_t step = (n + SAE_WAVE - 1) / SAE_WAVE, k = (uint32_t)__lane_id() * step;
+        const u64 in = __ballot(k < n && inside(lo + min(k, n - 1)));
+        const uint32_t skip = in ? (uint32_t)(63 - __builtin_clzll(in)) * step : 0;
+        lo += skip;
+        n = min(step, n - skip);
+    }
+    return logit_of(lo);
+}
+
 // Counts and masses up to each bin, itself included.
 template <int NW, int N>
 __device__ __forceinline__ void accumulate(Shared &s, u64 *mass, uint32_t *count)
@@ -320,17 +419,16 @@ __device__ __forceinline__ void accumulate(Shared &s, u64 *mass, uint32_t *count
     __syncthreads();
 }
 
-// The first i < n for which pred(i) holds (it holds from there on); n - 1 where none does.
-template <int THREADS, typename P>
-__device__ __forceinline__ int first_of(Shared &s, int n, P pred)
+// The first i < n <= 4096 for which pred(i) holds (it holds from there on); n - 1 where none does.  Every wave by itself.
+template <typename P>
+__device__ __forceinline__ int first_of(int n, P pred)
 {
-    __syncthreads();
-    if (threadIdx.x == 0) s.found = n - 1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += THREADS)
-        if (pred(i) && (i == 0 || !pred(i - 1))) s.found = i;
-    __syncthreads();
-    return uniform((int)s.found);
+    const int step = (n + SAE_WAVE - 1) / SAE_WAVE, lane = (int)__lane_id();
+    u64 in = __ballot(pred(min((lane + 1) * step, n) - 1));
+    if (!in) return n - 1;
+    const int from = __builtin_ctzll(in) * step;
+    in = __ballot(lane < step && pred(min(from + lane, n - 1)));
+    return min(from + __builtin_ctzll(in), n - 1);
 }
 
 // Sorts s.list[0 .. n - 1] and fills s.sums with the weights up to each, after `before`.
@@ -392,7 +490,7 @@ __device__ __forceinline__ Head locate(Shared &s, const Row<DT, THREADS> &row, c
 {
     constexpr int NW = THREADS / SAE_WAVE;
     auto reached = [&](u64 n, u64 mass) { return (by_count ? n : mass) >= target; };
-    const int b = first_of<THREADS>(s, BINS, [&](int i) { return reached(s.bins.count[i], s.bins.mass[i]); });
+    const int b = first_of(BINS, [&](int i) { return reached(s.bins.count[i], s.bins.mass[i]); });
     u64 n0 = b ? s.bins.count[b - 1] : 0, m0 = b ? s.bins.mass[b - 1] : 0;
     uint32_t left = s.bins.count[b] - (uint32_t)n0;
     if (by_count && b >= LIGHT) return {target, m0, 0, 0};  // (its tokens weigh nothing)
@@ -419,7 +517,7 @@ __device__ __forceinline__ Head locate(Shared &s, const Row<DT, THREADS> &row, c
         });
         __syncthreads();
         accumulate<NW, DIGITS>(s, s.digits.mass, s.digits.count);
-        const int d = first_of<THREADS>(s, DIGITS, [&](int i) { return reached(n0 + s.digits.count[i], m0 + s.digits.mass[i]); });
+        const int d = first_of(DIGITS, [&](int i) { return reached(n0 + s.digits.count[i], m0 + s.digits.mass[i]); });
         const uint32_t before = d ? s.digits.count[d - 1] : 0;
         left = s.digits.count[d] - before;
         m0 += d ? s.digits.mass[d - 1] : 0;
@@ -437,7 +535,7 @@ __device__ __forceinline__ Head locate(Shared &s, const Row<DT, THREADS> &row, c
         __syncthreads();
         const int n = uniform((int)s.n);
         sort_and_sum<NW>(s, sc, n, m0);
-        const int at = by_count ? min((int)(target - n0), n) - 1 : first_of<THREADS>(s, n, [&](int i) { return s.sums[i] >= target; });
+        const int at = by_count ? min((int)(target - n0), n) - 1 : first_of(n, [&](int i) { return s.sums[i] >= target; });
         const u64 sum = uniform64(s.sums[at]);
         return {n0 + at + 1, sum, sum - (at ? uniform64(s.sums[at - 1]) : m0), (uint32_t)uniform64(s.list[at])};
     }
@@ -459,12 +557,184 @@ __device__ __forceinline__ Head locate(Shared &s, const Row<DT, THREADS> &row, c
         });
         __syncthreads();
         accumulate<NW, DIGITS>(s, s.digits.mass, s.digits.count);
-        const int d = first_of<THREADS>(s, DIGITS, [&](int i) { return before + s.digits.count[i] >= r; });
+        const int d = first_of(DIGITS, [&](int i) { return before + s.digits.count[i] >= r; });
         before += d ? s.digits.count[d - 1] : 0;
         at |= (uint32_t)d << next;
     }
     h.index = at;
     return h;
+}
+
+// The answers from the bins that they can lie in; false where those hold too many tokens.
+// The questions are asked of the bins first, with bounds in place of the weight that the one before
+// leaves: each gives the bins of its answer and bounds for the next one.
+template <int DT, int THREADS, typename A>
+__device__ __forceinline__ bool answer_in_bins(Shared &s, const Row<DT, THREADS> &row, const Scale &sc, u64 kth, bool whole, float p,
+                                               float m, float u, A answer)
+{
+    constexpr int NW = THREADS / SAE_WAVE;
+    auto mass_of = [&](int b) { return b < 0 ? (u64)0 : uniform64(s.bins.mass[b]); };
+    auto count_of = [&](int b) { return b < 0 ? 0 : uniform((int)s.bins.count[b]); };
+    auto bin_of = [&](u64 mass) { return first_of(BINS, [&](int i) { return s.bins.mass[i] >= mass; }); };
+    int lo[4] = {-2, -2, -2, -2}, hi[4] = {-2, -2, -2, -2};  // of bins; rising and apart in the end
+    auto add = [&](int question, int x, int y) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < question; ++i)  // (takes in the ranges that it touches)
+            if (lo[i] >= 0 && lo[i] <= y + 1 && x <= hi[i] + 1) {
+                x = min(x, lo[i]);
+                y = max(y, hi[i]);
+                lo[i] = hi[i] = -2;
+            }
+        lo[question] = x;
+        hi[question] = y;
+    };
+    const u64 all = mass_of(BINS - 1);
+    u64 w0 = all, w1 = all;  // bounds of the weight that is left
+    int b0 = -1;
+    if (!whole) {
+        b0 = first_of(BINS, [&](int i) { return s.bins.count[i] >= kth; });
+        w0 = mass_of(b0 - 1);
+        w1 = mass_of(b0);
+        if (b0 < LIGHT) add(0, b0, b0);
+        else w0 = w1;  // (the light bin's tokens weigh nothing)
+        w0 = max(w0, (u64)ONE);
+    }
+    if (p < 1.0f) {
+        w0 = max(share(p, w0, true), (u64)ONE);
+        const u64 t1 = max(share(p, w1, true), (u64)ONE);
+        const int x = bin_of(w0), y = bin_of(t1);
+        add(1, x, y);
+        w1 = min(w1, mass_of(y));
+    }
+    int bm = -1;  // bins before bm weigh enough each, bins past bm + 2 do not
+    if (m > 0.0f) {
+        bm = max((int)fminf(-log2f(fminf(m, 1.0f)) * PER_TWO, (float)LIGHT) - 1, 0);
+        add(2, bm, bm + 2);
+        w0 = min(w0, max(mass_of(bm - 1), (u64)ONE));
+        w1 = min(w1, mass_of(bm + 2));
+    }
+    {
+        const int x = bin_of(drawn_at(u, w0) + 1), y = bin_of(drawn_at(u, w1) + 1);
+        add(3, x, y);
+    }
+    // in order; places in the list, and what lies before them in bins that are not in it
+#pragma unroll
+    for (int r = 0; r < 3; ++r)
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (lo[i] > lo[i + 1]) {
+                const int a = lo[i], b = hi[i];
+                lo[i] = lo[i + 1];
+                hi[i] = hi[i + 1];
+                lo[i + 1] = a;
+                hi[i + 1] = b;
+            }
+    int at[4], n = 0;
+    u64 gap[4], held = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        at[i] = n;
+        gap[i] = 0;
+        if (lo[i] < 0) continue;
+        gap[i] = mass_of(lo[i] - 1) - held;
+        n += count_of(hi[i]) - count_of(lo[i] - 1);
+        held += mass_of(hi[i]) - mass_of(lo[i] - 1);
+    }
+    if (n > LIST) return false;
+    __syncthreads();
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+    // the ranges' logits: from the lowest of its bins to below the lowest of the bins before
+    for (int t = threadIdx.x / SAE_WAVE; t < 8; t += NW) {
+        const int b = t & 1 ? lo[t / 2] - 1 : hi[t / 2];
+        const float x = lo[t / 2] < 0 ? __builtin_inff() : b < 0 ? __builtin_inff() : b >= LIGHT ? -0x1.fffffep127f : lowest_of(sc, b);
+        if (__lane_id() == 0) s.edges[t] = x;
+    }
+    __syncthreads();
+    float least[4], past[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        least[j] = s.edges[2 * j];
+        past[j] = s.edges[2 * j + 1];
+    }
+    uint32_t *indexes = reinterpret_cast<uint32_t *>(s.sums);
+    if (lo[2] < 0)  // uniform: one range
+        row.collect(indexes, &s.n, LIST, [&](float l) { return (l >= least[3]) & (l < past[3]); });
+    else
+        row.collect(indexes, &s.n, LIST, [&](float l) {
+            return ((l >= least[0]) & (l < past[0])) | ((l >= least[1]) & (l < past[1])) | ((l >= least[2]) & (l < past[2])) |
+                   ((l >= least[3]) & (l < past[3]));
+        });
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += THREADS) s.list[i] = (u64)key_of(row.logit((int)indexes[i])) << 32 | indexes[i];
+    __syncthreads();
+    sort_and_sum<NW>(s, sc, n, 0);
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        u64 g = gap[0];
+#pragma unroll
+        for (int j = 1; j < 4; ++j) g = lo[j] >= 0 && i >= at[j] ? gap[j] : g;
+        s.sums[i] += g;
+    }
+    __syncthreads();
+    auto weight_at = [&](int i) { return sc.weight(logit_of((uint32_t)(s.list[i] >> 32))); };
+    // tokens of the order before the list's token i
+    auto before = [&](int i) {
+        int b = 0, first = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (lo[j] >= 0 && i >= at[j]) {
+                b = count_of(lo[j] - 1);
+                first = at[j];
+            }
+        return b + i - first;
+    };
+    u64 kept = kth, w = all;
+    if (!whole) {
+        if (b0 >= LIGHT) w = all;
+        else {
+            int i = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (lo[j] >= 0 && lo[j] <= b0) i = at[j] + (int)kth - 1 - count_of(lo[j] - 1);
+            w = uniform64(s.sums[i]);
+        }
+    }
+    if (p < 1.0f) {
+        const u64 target = max(share(p, w, true), 1ull);
+        const int i = first_of(n, [&](int i) { return s.sums[i] >= target; });
+        w = uniform64(s.sums[i]);
+        kept = before(i) + 1;
+    }
+    if (m > 0.0f) {
+        const double least = (double)m * ONE;
+        int from = 0, to = 0;  // the list's tokens of bins bm .. bm + 2
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (lo[j] >= 0 && lo[j] <= bm && hi[j] >= bm + 2) {
+                from = at[j] + count_of(bm - 1) - count_of(lo[j] - 1);
+                to = at[j] + count_of(bm + 2) - count_of(lo[j] - 1);
+            }
+        __syncthreads();
+        if (threadIdx.x == 0) s.found = to;
+        __syncthreads();
+        for (int i = from + threadIdx.x; i < to; i += THREADS)
+            if ((double)weight_at(i) < least) atomicMin(&s.found, (uint32_t)i);
+        __syncthreads();
+        const int i = uniform((int)s.found);  // the first that weighs too little
+        u64 c = count_of(bm - 1) + i - from, mass = i > from ? uniform64(s.sums[i - 1]) : mass_of(bm - 1);
+        if (c == 0) {
+            c = 1;
+            mass = (u64)ONE;
+        }
+        if (c < kept) {
+            kept = c;
+            w = mass;
+        }
+    }
+    const u64 target = drawn_at(u, w);
+    const int i = first_of(n, [&](int i) { return s.sums[i] > target; });
+    if (threadIdx.x == 0) answer((uint32_t)s.list[i], (float)((double)weight_at(i) / (double)w), (uint32_t)kept);
+    return true;
 }
 
 template <int DT, int THREADS>
@@ -562,16 +832,18 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
         if (threadIdx.x == 0) s.n = 0;
         __syncthreads();
         uint32_t light = 0;
-        row.each([&](float l, int) {
-            double rest;
-            const int b = sc.split(l, rest);
-            if (b < LIGHT) {
-                atomicAdd(&s.bins.count[b], 1u);
-                atomicAdd(&s.bins.mass[b], sc.weight(b, rest));
-            } else {
-                light += l > LOWEST;
-            }
-        });
+        row.each(row.any_below(sc.floor_of(LIGHT)),
+                 [&](float l, int) {
+                     double rest;
+                     const int b = sc.split(l, rest);
+                     if (b < LIGHT) {
+                         atomicAdd(&s.bins.count[b], 1u);
+                         atomicAdd(&s.bins.mass[b], sc.weight(b, rest));
+                     } else {
+                         light += l > LOWEST;
+                     }
+                 },
+                 [&](float l) { light += l > LOWEST; });
         light = sum_upto(light);
         if (lane == SAE_WAVE - 1 && light) atomicAdd(&s.bins.count[LIGHT], light);
         __syncthreads();
@@ -580,23 +852,27 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
         total = s.bins.mass[BINS - 1];
         kth = k > 0 && (uint32_t)k < all ? (uint32_t)k : all;
         whole = kth == all;
-        int last = whole ? LIGHT : first_of<THREADS>(s, BINS, [&](int i) { return s.bins.count[i] >= kth; });
+        int last = whole ? LIGHT : first_of(BINS, [&](int i) { return s.bins.count[i] >= kth; });
         // (top-p of what top-k leaves: its weight has to be known first)
         if (whole && p < 1.0f) {
             const u64 most = share(p, total, true);
-            last = first_of<THREADS>(s, BINS, [&](int i) { return s.bins.mass[i] >= most; });
+            last = first_of(BINS, [&](int i) { return s.bins.mass[i] >= most; });
         }
         if (m > 0.0f && (whole || !(p < 1.0f))) {
             const float x = -log2f(fminf(m, 1.0f)) * PER_TWO + 2.0f;
             if (x < (float)last) last = (int)x;
         }
         n = (int)s.bins.count[last];
-        if (n <= LIST) {
+        if (n <= SAE_WAVE) {
             const float least = last >= LIGHT - 1 ? -0x1.fffffep127f : sc.floor_of(last);
             row.some(least, [&](float l, int i) {
                 if (l >= least && sc.bin(l) <= last) s.list[min(atomicAdd(&s.n, 1u), (uint32_t)LIST - 1)] = (u64)key_of(l) << 32 | (uint32_t)i;
             });
             __syncthreads();
+        } else if (answer_in_bins(s, row, sc, kth, whole, p, m, u, answer)) {
+            return;
+        } else {
+            n = LIST + 1;
         }
     }
     if (n <= SAE_WAVE) {  // one wave, a token a lane
@@ -629,16 +905,16 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
         int keep = k > 0 ? min(k, n) : n;
         if (p < 1.0f) {
             const u64 target = share(p, whole ? total : uniform64(s.sums[keep - 1]), true);
-            keep = first_of<THREADS>(s, keep, [&](int i) { return s.sums[i] >= target; }) + 1;
+            keep = first_of(keep, [&](int i) { return s.sums[i] >= target; }) + 1;
         }
         if (m > 0.0f) {
             const double least = (double)m * ONE;
             auto light = [&](int i) { return (double)(s.sums[i] - (i ? s.sums[i - 1] : 0)) < least; };
-            const int at = first_of<THREADS>(s, keep, light);
+            const int at = first_of(keep, light);
             if (light(at)) keep = max(at, 1);
         }
         const u64 of = uniform64(s.sums[keep - 1]), target = drawn_at(u, of);
-        const int at = first_of<THREADS>(s, keep, [&](int i) { return s.sums[i] > target; });
+        const int at = first_of(keep, [&](int i) { return s.sums[i] > target; });
         if (threadIdx.x == 0) answer((uint32_t)s.list[at], (float)((double)(s.sums[at] - (at ? s.sums[at - 1] : 0)) / (double)of), keep);
         return;
     }
