@@ -11,6 +11,12 @@
 // A workgroup takes a part of a tile (one sequence's tokens of one page): it computes the cosines and sines
 // of the tile's tokens once into LDS, for all of its heads, then each thread takes 4 tokens x
 // two 16-byte pieces, the two that hold the pairs' halves, of keys and values or of queries.
+//
+// Bound by memory: 22,600 tokens of 32 and 8 heads of 128 into an 8-bit cache, 124 us: 509 MB (272
+// fetched, 227 written, by the counters), 4.1 TB/s, where a copy reaches 5.1.  At 128 registers,
+// four waves a SIMD (180, two waves: 141 us; the next rows or the first ones loaded ahead of the angles:
+// spilled, 145 and more; 2, 3 or 5 items a thread: 121 to 127).  A step of 256 tokens is 8.2 us, one token 5.9: dependent round
+// trips (sequence, table entry, positions, rows).
 #include "kv_page.h"
 
 namespace {
@@ -110,76 +116,83 @@ __device__ __forceinline__ uint32_t quantise2(const float (&a)[8], const float (
     return byte;
 }
 
-// Keys or values of 4 tokens, 2 pieces each, into the page.
-template <int TYPE, int D, int DT, bool VALUES>
-__device__ __forceinline__ void put(const KvDev &c, const Place &p, int head, int tg, int lane, const int (&ch)[2],
-                                    const float (&x)[4][2][8])
+// A token's turned keys, 2 pieces, into the page.
+template <int TYPE, int D, int DT>
+__device__ __forceinline__ void put_key(const KvDev &c, const Place &p, int head, int t, int lane, const int (&ch)[2], bool turned,
+                                        const u32x4 (&raw)[2], const float (&x)[8], const float (&y)[8])
 {
     constexpr int E = TYPE == SAE_KV_FP8 ? 1 : 2;
-    char *page = (VALUES ? c.v : c.k) + p.block * c.block_bytes + (int64_t)head * (SAE_KV_BLOCK * D * E);
-    u32x4 w[4][2];  // 8-bit: the first two words
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = tg * 4 + i;
-        if constexpr (TYPE == SAE_KV_FP8) {
-            u32x2 a, b;
-            const uint32_t byte = quantise2<D / 16>(x[i][0], x[i][1], a, b);
-            w[i][0] = u32x4{a[0], a[1], 0, 0};
-            w[i][1] = u32x4{b[0], b[1], 0, 0};
-            if (lane == 0 && t >= p.t_lo && t < p.t_hi)
-                (VALUES ? c.vs : c.ks)[p.block * c.scale_stride + head * SAE_KV_BLOCK + t] = (uint8_t)byte;
-        } else {
-            w[i][0] = round8<DT>(x[i][0]);
-            w[i][1] = round8<DT>(x[i][1]);
-        }
+    char *page = c.k + p.block * c.block_bytes + (int64_t)head * (SAE_KV_BLOCK * D * E);
+    const bool there = t >= p.t_lo && t < p.t_hi;
+    if constexpr (TYPE == SAE_KV_FP8) {
+        u32x2 a, b;
+        const uint32_t byte = quantise2<D / 16>(x, y, a, b);
+        if (!there) return;
+        *reinterpret_cast<u32x2 *>(page + (ch[0] / 2) * 256 + t * 16 + (ch[0] & 1) * 8) = a;
+        *reinterpret_cast<u32x2 *>(page + (ch[1] / 2) * 256 + t * 16 + (ch[1] & 1) * 8) = b;
+        if (lane == 0) c.ks[p.block * c.scale_stride + head * SAE_KV_BLOCK + t] = (uint8_t)byte;
+    } else {
+        if (!there) return;
+        *reinterpret_cast<u32x4 *>(page + ch[0] * 256 + t * 16) = turned ? round8<DT>(x) : raw[0];
+        *reinterpret_cast<u32x4 *>(page + ch[1] * 256 + t * 16) = turned ? round8<DT>(y) : raw[1];
     }
-    if constexpr (!VALUES) {
+}
+
+// Values of 4 tokens, 2 pieces each, into the page.
+template <int TYPE, int D, int DT>
+__device__ __forceinline__ void put_values(const KvDev &c, const Place &p, int head, int tg, int lane, const int (&ch)[2],
+                                           const u32x4 (&raw)[4][2])
+{
+    constexpr int E = TYPE == SAE_KV_FP8 ? 1 : 2;
+    char *page = c.v + p.block * c.block_bytes + (int64_t)head * (SAE_KV_BLOCK * D * E);
+    const bool whole = tg * 4 >= p.t_lo && tg * 4 + 4 <= p.t_hi;
+    if constexpr (TYPE == SAE_KV_FP8) {
+        u32x2 q[4][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = tg * 4 + i;
-            if (t < p.t_lo || t >= p.t_hi) continue;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if constexpr (TYPE == SAE_KV_FP8)
-                    *reinterpret_cast<u32x2 *>(page + (ch[u] / 2) * 256 + t * 16 + (ch[u] & 1) * 8) = u32x2{w[i][u][0], w[i][u][1]};
-                else
-                    *reinterpret_cast<u32x4 *>(page + ch[u] * 256 + t * 16) = w[i][u];
-            }
+            float x[8], y[8];
+            widen<DT>(raw[i][0], x);
+            widen<DT>(raw[i][1], y);
+            const uint32_t byte = quantise2<D / 16>(x, y, q[i][0], q[i][1]);
+            if (lane == 0 && t >= p.t_lo && t < p.t_hi) c.vs[p.block * c.scale_stride + head * SAE_KV_BLOCK + t] = (uint8_t)byte;
         }
-    } else {
-        const bool whole = tg * 4 >= p.t_lo && tg * 4 + 4 <= p.t_hi;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 char *to = page + v_unit<TYPE>(ch[u] * 8 + j, tg);
-                if constexpr (TYPE == SAE_KV_FP8) {
-                    uint32_t y = 0;
+                uint32_t y = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) y |= ((w[i][u][j / 4] >> (8 * (j & 3))) & 0xFFu) << (8 * i);
-                    if (whole) *reinterpret_cast<uint32_t *>(to) = y;
-                    else {
+                for (int i = 0; i < 4; ++i) y |= ((q[i][u][j / 4] >> (8 * (j & 3))) & 0xFFu) << (8 * i);
+                if (whole) *reinterpret_cast<uint32_t *>(to) = y;
+                else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (tg * 4 + i >= p.t_lo && tg * 4 + i < p.t_hi) to[i] = (char)(y >> (8 * i));
-                    }
-                } else {
-                    uint32_t h[4];
+                    for (int i = 0; i < 4; ++i)
+                        if (tg * 4 + i >= p.t_lo && tg * 4 + i < p.t_hi) to[i] = (char)(y >> (8 * i));
+                }
+            }
+    } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) h[i] = (w[i][u][j / 2] >> (16 * (j & 1))) & 0xFFFFu;
-                    if (whole) *reinterpret_cast<u32x2 *>(to) = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
-                    else {
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (tg * 4 + i >= p.t_lo && tg * 4 + i < p.t_hi) reinterpret_cast<uint16_t *>(to)[i] = (uint16_t)h[i];
-                    }
+            for (int j = 0; j < 8; ++j) {
+                char *to = page + v_unit<TYPE>(ch[u] * 8 + j, tg);
+                uint32_t h[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[i] = (raw[i][u][j / 2] >> (16 * (j & 1))) & 0xFFFFu;
+                if (whole) *reinterpret_cast<u32x2 *>(to) = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+                else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (tg * 4 + i >= p.t_lo && tg * 4 + i < p.t_hi) reinterpret_cast<uint16_t *>(to)[i] = (uint16_t)h[i];
                 }
             }
     }
 }
 
 template <int TYPE, int D, int DT>
-__global__ void __launch_bounds__(THREADS) k_kv_append(KvDev c, Append a)
+__global__ void __launch_bounds__(THREADS, 4) k_kv_append(KvDev c, Append a)
 {
     constexpr int LANES = D / 16;  // of a token's row
     __shared__ float2 cs[SAE_KV_BLOCK][D / 2];
@@ -202,60 +215,61 @@ __global__ void __launch_bounds__(THREADS) k_kv_append(KvDev c, Append a)
         cs[t][j] = circle((double)pos * ((double)a.freq[j] * 0.159154943091895335769), a.factor);
     }
     __syncthreads();
+#pragma unroll 1
     for (int at = start; at < items; at += step) {
         const bool query = at >= kv_items;
         const int n = query ? at - kv_items : at, lane = n % LANES, g = n / LANES;
         const int head = (int)((uint32_t)g / (uint32_t)groups), tg = tg0 + g - head * groups;
-        // the lane's two pieces, and its first pair
+        // the lane's two pieces
         const int h8 = half / 8;
         const bool turned = lane < h8, apart = turned && !a.interleaved;
         const int ch[2] = {apart ? lane : 2 * lane, apart ? lane + h8 : 2 * lane + 1};
-        const uint16_t *from = query ? a.q : a.k;
-        const int64_t stride = query ? a.q_stride : a.k_stride;
         if (!query && p.block < 0) continue;
-        u32x4 xk[4][2], xv[4][2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = tg * 4 + i;
-            const int64_t row = (int64_t)p.row0 + t;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                xk[i][u] = xv[i][u] = u32x4{0, 0, 0, 0};
-                if (t >= p.t_lo && t < p.t_hi) {
-                    xk[i][u] = *reinterpret_cast<const u32x4 *>(from + row * stride + head * D + ch[u] * 8);
-                    if (!query) xv[i][u] = *reinterpret_cast<const u32x4 *>(a.v + row * a.v_stride + head * D + ch[u] * 8);
-                }
-            }
-        }
-        float x[4][2][8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            widen<DT>(xk[i][0], x[i][0]);
-            widen<DT>(xk[i][1], x[i][1]);
-            const int t = tg * 4 + i;
-            if (turned && t >= p.t_lo && t < p.t_hi) {
-                if (a.interleaved) turn(x[i][0], x[i][1], cs[t], lane * 8, true);
-                else turn(x[i][0], x[i][1], cs[t], lane * 8, false);
-            }
-        }
-        if (query) {
+        auto load = [&](u32x4 (&x)[4][2], const uint16_t *from, int64_t stride) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int t = tg * 4 + i;
+                const uint16_t *row = from + ((int64_t)p.row0 + t) * stride + head * D;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    x[i][u] = u32x4{0, 0, 0, 0};
+                    if (t >= p.t_lo && t < p.t_hi) x[i][u] = *reinterpret_cast<const u32x4 *>(row + ch[u] * 8);
+                }
+            }
+        };
+        auto turn_token = [&](const u32x4 (&raw)[2], int t, float (&x)[8], float (&y)[8]) __attribute__((always_inline)) {
+            widen<DT>(raw[0], x);
+            widen<DT>(raw[1], y);
+            if (turned && t >= p.t_lo && t < p.t_hi) {
+                if (a.interleaved) turn(x, y, cs[t], lane * 8, true);
+                else turn(x, y, cs[t], lane * 8, false);
+            }
+        };
+        if (query) {
+            u32x4 raw[4][2];
+            load(raw, a.q, a.q_stride);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = tg * 4 + i;
+                float x[8], y[8];
+                turn_token(raw[i], t, x, y);
                 if (t < p.t_lo || t >= p.t_hi) continue;
                 uint16_t *to = a.q_out + ((int64_t)p.row0 + t) * a.out_stride + head * D;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) *reinterpret_cast<u32x4 *>(to + ch[u] * 8) = turned ? round8<DT>(x[i][u]) : xk[i][u];
+                *reinterpret_cast<u32x4 *>(to + ch[0] * 8) = turned ? round8<DT>(x) : raw[i][0];
+                *reinterpret_cast<u32x4 *>(to + ch[1] * 8) = turned ? round8<DT>(y) : raw[i][1];
             }
             continue;
         }
-        put<TYPE, D, DT, false>(c, p, head, tg, lane, ch, x);
+        u32x4 rk[4][2], rv[4][2];
+        load(rk, a.k, a.k_stride);
+        load(rv, a.v, a.v_stride);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            widen<DT>(xv[i][0], x[i][0]);
-            widen<DT>(xv[i][1], x[i][1]);
+            float x[8], y[8];
+            turn_token(rk[i], tg * 4 + i, x, y);
+            put_key<TYPE, D, DT>(c, p, head, tg * 4 + i, lane, ch, turned, rk[i], x, y);
         }
-        put<TYPE, D, DT, true>(c, p, head, tg, lane, ch, x);
+        put_values<TYPE, D, DT>(c, p, head, tg, lane, ch, rv);
     }
 }
 
