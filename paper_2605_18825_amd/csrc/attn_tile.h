@@ -108,6 +108,38 @@ __device__ __forceinline__ long long uniform(long long x)
     return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
+typedef unsigned long long u64;
+
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ uint32_t moved(uint32_t idle, uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)idle, (int)x, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ u64 moved(u64 idle, u64 x)
+{
+    return (u64)moved<CTRL, ROWS>((uint32_t)(idle >> 32), (uint32_t)(x >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)idle, (uint32_t)x);
+}
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ float moved(float idle, float x)
+{
+    return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(idle), __float_as_uint(x)));
+}
+
+// f over lanes 0 .. this one, by moves within rows of 16 lanes and from row to row; `idle` changes nothing.
+template <typename T, typename F>
+__device__ __forceinline__ T upto(T x, T idle, F f)
+{
+    x = f(x, moved<0x111>(idle, x));        // row_shr 1, 2, 4, 8
+    x = f(x, moved<0x112>(idle, x));
+    x = f(x, moved<0x114>(idle, x));
+    x = f(x, moved<0x118>(idle, x));
+    x = f(x, moved<0x142, 0xA>(idle, x));   // the rows' last lanes into the rows behind
+    return f(x, moved<0x143, 0xC>(idle, x));
+}
+template <typename T>
+__device__ __forceinline__ T sum_upto(T x) { return upto(x, (T)0, [](T a, T b) { return a + b; }); }
+
 // Exclusive scan over a workgroup of NW waves; total in every thread.  lds: NW
 // values that nothing else uses.
 template <int NW, typename T>

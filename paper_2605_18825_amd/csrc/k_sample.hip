@@ -21,7 +21,9 @@
 
 namespace {
 
+using attn::sum_upto;
 using attn::uniform;
+using attn::upto;
 
 constexpr int LIST = 2048;           // tokens that are sorted in LDS
 constexpr int PER_TWO = 32;          // bins of a factor of two in weight
@@ -30,7 +32,7 @@ constexpr int BINS = 1536, DIGITS = 1024;
 constexpr int GROUPS = 16;           // of a thread's logits
 constexpr double ONE = 8796093022208.0;  // 2^43
 constexpr float LOWEST = -__builtin_inff();
-typedef unsigned long long u64;
+typedef attn::u64 u64;
 static_assert(LIGHT < BINS, "");
 
 struct Args {
@@ -44,36 +46,6 @@ struct Args {
 };
 
 // ------------------------------------------------------------- waves and workgroups
-template <int CTRL, int ROWS = 0xF>
-__device__ __forceinline__ uint32_t moved(uint32_t idle, uint32_t x)
-{
-    return (uint32_t)__builtin_amdgcn_update_dpp((int)idle, (int)x, CTRL, ROWS, 0xF, false);
-}
-template <int CTRL, int ROWS = 0xF>
-__device__ __forceinline__ u64 moved(u64 idle, u64 x)
-{
-    return (u64)moved<CTRL, ROWS>((uint32_t)(idle >> 32), (uint32_t)(x >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)idle, (uint32_t)x);
-}
-template <int CTRL, int ROWS = 0xF>
-__device__ __forceinline__ float moved(float idle, float x)
-{
-    return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(idle), __float_as_uint(x)));
-}
-
-// f over lanes 0 .. this one, by moves within rows of 16 lanes and from row to row; `idle` changes nothing.
-template <typename T, typename F>
-__device__ __forceinline__ T upto(T x, T idle, F f)
-{
-    x = f(x, moved<0x111>(idle, x));        // row_shr 1, 2, 4, 8
-    x = f(x, moved<0x112>(idle, x));
-    x = f(x, moved<0x114>(idle, x));
-    x = f(x, moved<0x118>(idle, x));
-    x = f(x, moved<0x142, 0xA>(idle, x));   // the rows' last lanes into the rows behind
-    return f(x, moved<0x143, 0xC>(idle, x));
-}
-template <typename T>
-__device__ __forceinline__ T sum_upto(T x) { return upto(x, (T)0, [](T a, T b) { return a + b; }); }
-
 __device__ __forceinline__ uint32_t of_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 __device__ __forceinline__ u64 of_lane(u64 x, int lane) { return (u64)of_lane((uint32_t)(x >> 32), lane) << 32 | of_lane((uint32_t)x, lane); }
 __device__ __forceinline__ float of_lane(float x, int lane) { return __uint_as_float(of_lane(__float_as_uint(x), lane)); }

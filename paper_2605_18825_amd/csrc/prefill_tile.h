@@ -164,14 +164,11 @@ struct Part {
 };
 constexpr int PER_THREAD = 2;  // sequences of a thread at most: no more than tiles, which are 512 at most
 
-// A tree's call may have many more tiles than workgroups are wanted: parts are numbered in the
-// workspace among those of split tiles alone.  (Such a tile's keys are 3/2 shares at least and its parts at
-// most 4/3 as many as shares: 4/3 groups in all, of the 2 groups that there are.)
-template <int NW, bool TREE>
+template <int NW>
 __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, const Plan &plan, int x, int rows, int keys)
 {
-    __shared__ long long tmp[TREE ? 3 : 2][NW], found_rest;
-    __shared__ int found_seq, found_parts, found_slot;
+    __shared__ long long tmp[2][NW], found_rest;
+    __shared__ int found_seq, found_parts;
     const int G = a.heads / c.kvh, chunk = (c.n_seq + NW * SAE_WAVE - 1) / (NW * SAE_WAVE);
     // tiles of sequence r, and the mean of their steps, about
     auto size = [&](int r, int &tiles, int &steps) {
@@ -184,14 +181,11 @@ __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, con
     auto share_of = [&](long long total) {
         return (int)max((total + plan.groups - 1) / plan.groups, (long long)(MIN_SPLIT / keys));
     };
-    auto parts_of_share = [&](int steps, int share) { return min(max((steps + (TREE ? share / 2 : 0)) / share, 1), plan.most); };
     if (c.n_seq == 1) {  // uniform: no scans
         int tiles, steps;
         size(0, tiles, steps);
-        const int parts = parts_of_share(steps, share_of((long long)tiles * steps));
-        const bool there = x < (long long)tiles * parts;
-        const bool held = there && parts > 1;
-        return {there ? 0 : -1, x % parts, parts, x / parts, TREE && !held ? -1 : x, TREE && !held ? x : -1};
+        const int parts = min(max(steps / share_of((long long)tiles * steps), 1), plan.most);
+        return {x < (long long)tiles * parts ? 0 : -1, x % parts, parts, x / parts, x, -1};
     }
     const int r0 = min((int)threadIdx.x * chunk, c.n_seq);
     int tiles[PER_THREAD], steps[PER_THREAD];
@@ -207,15 +201,13 @@ __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, con
     long long total;
     scan<NW>(work, total, tmp[0]);
     const int share = share_of(total);
-    long long count = 0, held = 0, all_held = 0, held_before = 0;
+    long long count = 0;
 #pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
-        steps[i] = parts_of_share(steps[i], share);  // parts from here on
+        steps[i] = min(max(steps[i] / share, 1), plan.most);  // parts from here on
         count += (long long)tiles[i] * steps[i];
-        if (TREE && steps[i] > 1) held += (long long)tiles[i] * steps[i];
     }
     long long before = scan<NW>(count, total, tmp[1]);
-    if constexpr (TREE) held_before = scan<NW>(held, all_held, tmp[2]);
     if (x >= before && x < before + count) {  // one thread
 #pragma unroll
         for (int i = 0; i < PER_THREAD; ++i) {
@@ -224,17 +216,96 @@ __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, con
                 found_seq = r0 + i;
                 found_parts = steps[i];
                 found_rest = x - before;
-                if (TREE) found_slot = steps[i] > 1 ? (int)(held_before + x - before) : -1;
             }
             before += k;
-            if (TREE && steps[i] > 1) held_before += k;
         }
     }
     __syncthreads();
-    const int clear = TREE && x >= all_held ? x : -1;
-    if (x >= total) return {-1, 0, 1, 0, -1, clear};
+    if (x >= total) return {-1, 0, 1, 0, x, -1};
     const int parts = uniform(found_parts), rest = uniform((int)found_rest);
-    return {uniform(found_seq), rest % parts, parts, rest / parts, TREE ? uniform(found_slot) : x, clear};
+    return {uniform(found_seq), rest % parts, parts, rest / parts, x, -1};
+}
+
+// A tree's call may have many more tiles than workgroups are wanted: parts are numbered in the
+// workspace among those of split tiles alone.  (Such a tile's keys are 3/2 shares at least and its parts at
+// most 4/3 as many as shares: 4/3 groups in all, of the 2 groups that there are.)
+template <int NW>
+__device__ __forceinline__ Part find_part_tree(const KvDev &c, const AttnArgs &a, const Plan &plan, int x, int rows, int keys)
+{
+    __shared__ u64 sums[2][NW], found;
+    __shared__ int found_seq, found_rest;
+    const int G = a.heads / c.kvh, chunk = (c.n_seq + NW * SAE_WAVE - 1) / (NW * SAE_WAVE);
+    const int lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
+    // tiles of sequence r, and their steps
+    auto size = [&](int r, int &tiles, int &steps) {
+        int first, tokens;
+        kv::seq_rows(c, r, first, tokens);
+        const int len = kv::seq_len(c, r);
+        tiles = (int)((uint32_t)(tokens * G + rows - 1) / (uint32_t)rows);
+        steps = (a.window > 0 ? min(a.window + tokens, len) : len) / keys + 1;
+    };
+    // (in floating point: a quotient of 64-bit numbers is some hundred instructions; at least the quotient)
+    auto parts_of = [&](u64 total, int steps) {
+        const int share = max((int)((double)total / plan.groups) + 1, MIN_SPLIT / keys);
+        return min(max((int)((uint32_t)(steps + share / 2) / (uint32_t)share), 1), plan.most);
+    };
+    if (c.n_seq == 1) {  // uniform
+        int tiles, steps;
+        size(0, tiles, steps);
+        const int parts = parts_of((u64)tiles * steps, steps), sub = (int)((uint32_t)x / (uint32_t)parts);
+        const bool held = sub < tiles && parts > 1;
+        return {sub < tiles ? 0 : -1, x - sub * parts, parts, sub, held ? x : -1, held ? -1 : x};
+    }
+    const int r0 = min((int)threadIdx.x * chunk, c.n_seq);
+    int tiles[PER_THREAD], steps[PER_THREAD];
+    u64 work = 0;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+        tiles[i] = steps[i] = 0;
+        if (i < chunk && r0 + i < c.n_seq) {
+            size(r0 + i, tiles[i], steps[i]);
+            work += (u64)tiles[i] * steps[i];
+        }
+    }
+    work = sum_upto(work);
+    if (lane == SAE_WAVE - 1) sums[0][wave] = work;
+    __syncthreads();
+    u64 total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) total += sums[0][w];
+    // workgroups (upper word) and places in the workspace
+    u64 count = 0;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+        steps[i] = parts_of(total, steps[i]);  // parts from here on
+        const u64 k = (u64)tiles[i] * steps[i];
+        count += k << 32 | (steps[i] > 1 ? k : 0);
+    }
+    const u64 upto_here = sum_upto(count);
+    if (lane == SAE_WAVE - 1) sums[1][wave] = upto_here;
+    __syncthreads();
+    u64 before = upto_here - count, all = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        before += w < wave ? sums[1][w] : 0;
+        all += sums[1][w];
+    }
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+        const u64 k = (u64)tiles[i] * steps[i];
+        const int rest = x - (int)(before >> 32);
+        if (rest >= 0 && rest < (int)k) {  // one thread
+            found_seq = r0 + i;
+            found_rest = rest;
+            found = (u64)(uint32_t)steps[i] << 32 | (steps[i] > 1 ? (uint32_t)before + (uint32_t)rest : ~0u);
+        }
+        before += k << 32 | (steps[i] > 1 ? k : 0);
+    }
+    __syncthreads();
+    const int clear = x >= (int)(uint32_t)all ? x : -1;
+    if (x >= (int)(all >> 32)) return {-1, 0, 1, 0, -1, clear};
+    const int parts = uniform((int)(found >> 32)), rest = uniform(found_rest), sub = (int)((uint32_t)rest / (uint32_t)parts);
+    return {uniform(found_seq), rest - sub * parts, parts, sub, uniform((int)(uint32_t)found), clear};
 }
 
 // A split tile as the workspace has it, by the workgroup of its first part.
@@ -311,6 +382,35 @@ __device__ __forceinline__ void fill_masks(const KvDev &c, const AttnArgs &a, co
         if (c.status) atomicOr(c.status, (uint32_t)SAE_ST_BAD_TREE);
         parent = -1;
     }
+    if (n <= SAE_WAVE) {  // uniform: a wave by itself, its lanes' rows in registers
+        if (threadIdx.x < SAE_WAVE) {
+            u64 row = live ? 1ull << j : 0, near = 0;
+            int up = live ? parent : -1, count = 1, at = live ? j : -1;
+#pragma unroll 1
+            for (int k = 0;; ++k) {
+                if (hops >> k & 1) {  // uniform
+                    const u64 more = __shfl(row, max(at, 0));
+                    const int next = __shfl(up, max(at, 0));
+                    near |= at >= 0 ? more : 0;
+                    at = at >= 0 ? next : -1;
+                }
+                if (1 << k >= n) break;
+                const u64 more = __shfl(row, max(up, 0));
+                const int next = __shfl(up, max(up, 0)), tokens = __shfl(count, max(up, 0));
+                row |= up >= 0 ? more : 0;
+                count += up >= 0 ? tokens : 0;
+                up = up >= 0 ? next : -1;
+            }
+            if (hops) row = near;
+            m.seen[j][0] = (uint32_t)row;
+            m.seen[j][1] = (uint32_t)(row >> 32);
+#pragma unroll
+            for (int w = 2; w < MASK_WORDS; ++w) m.seen[j][w] = 0;
+            m.count[j] = count;
+        }
+        __syncthreads();
+        return;
+    }
     uint32_t row[MASK_WORDS], near[MASK_WORDS];
 #pragma unroll
     for (int w = 0; w < MASK_WORDS; ++w) {
@@ -355,16 +455,16 @@ __device__ __forceinline__ void fill_masks(const KvDev &c, const AttnArgs &a, co
     }
 }
 
-// The wave's rows over steps s0 .. s1 - 1 once more, one key at a time on the
+// The wave's rows over keys key0 .. key1 - 1 once more, one key at a time on the
 // vector units, each row adding the keys it sees and no other: the slow path
 // for values that are not finite and that not all of the rows see, and for scores past
 // 2^24 (about 130 times as long as the loop it replaces, with the same state after it).
 template <int TYPE, int D, bool TREE>
-__device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, const Masks *masks, int64_t base, int kvhead, int s0,
-                     int s1, int token, int head, int pos, f32x16 (&o)[D / 32], float &m, float &l)
+__device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, const Masks *masks, int64_t base, int kvhead, int key0,
+                     int key1, int token, int head, int pos, f32x16 (&o)[D / 32], float &m, float &l)
 {
     constexpr bool FP8 = TYPE == SAE_KV_FP8, F16 = is_f16(TYPE);
-    constexpr int E = FP8 ? 1 : 2, PAGE = SAE_KV_BLOCK * D * E, ND = FP8 ? 2 : 1, KEYS = keys_of(D);
+    constexpr int E = FP8 ? 1 : 2, PAGE = SAE_KV_BLOCK * D * E, ND = FP8 ? 2 : 1;
     const int h = (int)__lane_id() >> 5;
     const int lo = a.window > 0 ? max(0, (TREE ? t.pos0 + masks->count[token] - 1 : pos) - a.window + 1) : 0;
     const uint16_t *q = static_cast<const uint16_t *>(a.q) + (int64_t)(t.first + token) * a.q_stride + (int64_t)head * D;
@@ -375,7 +475,7 @@ __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, const Mas
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
 #pragma unroll 1
-    for (int key = s0 * KEYS; key < min(s1 * KEYS, t.len); ++key) {
+    for (int key = key0; key < key1; ++key) {
         const int id = c.ids[(int64_t)t.seq * c.max_blocks + key / SAE_KV_BLOCK], tk = key % SAE_KV_BLOCK;
         if (base < 0 || id < 0 || id >= c.bpi) continue;  // uniform
         const char *kp = c.k + (base + id) * c.block_bytes + (int64_t)kvhead * PAGE;
@@ -475,7 +575,7 @@ __device__ __forceinline__ void finish(const KvDev &c, const AttnArgs &a, const 
         const int p1 = t.pos0 + t.token0 + (t.head0 + min(wave * ROWS + ROWS, t.rows) - 1) / G;
         if (__any(live && huge) || any_odd<TYPE, D>(c, t, base, kvhead, max(p0 + 1, k0), k1) ||
             (a.window > 0 && any_odd<TYPE, D>(c, t, base, kvhead, k0, min(p1 - a.window + 1, k1))))
-            redo<TYPE, D, TREE>(c, a, t, masks, base, kvhead, s0, s1, token, head, live ? t.pos0 + token : -1, o, m, l);
+            redo<TYPE, D, TREE>(c, a, t, masks, base, kvhead, k0, k1, token, head, live ? t.pos0 + token : -1, o, m, l);
     }
 
     l += __shfl_xor(l, 32);
@@ -540,7 +640,9 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
     Tile t;
     int part = 0, nparts = 1, slot = x;
     if constexpr (SPLIT) {
-        const Part p = find_part<NW, TREE>(c, a, plan, x, NW * ROWS, KEYS);
+        Part p;
+        if constexpr (TREE) p = find_part_tree<NW>(c, a, plan, x, NW * ROWS, KEYS);
+        else p = find_part<NW>(c, a, plan, x, NW * ROWS, KEYS);
         if (p.seq >= 0) t = tile_of<TREE>(c, a, p.seq, p.sub, NW * ROWS, KEYS);
         slot = p.slot;
         if constexpr (TREE) {
