@@ -94,6 +94,7 @@ struct Plan {
                  // keys are split; 0: none is
     int most;    // parts of a tile at most (from the keys that the table holds)
     int slots;   // parts that the workspace holds
+    int joins;   // a tree's call: split tiles at most
 };
 
 // The rows of a workgroup and the keys they see.
@@ -160,7 +161,9 @@ struct Part {
     int seq, part, parts;  // seq < 0: none
     int sub;
     int slot;  // the part's place in the workspace, -1 for none
-    int clear; // a place there that no part has, for this workgroup to say so; -1 for none
+    // trees: the tile's number among those that are split, for its first part to note (-1: not this one), and
+    // a number that no tile has, for this workgroup to say so
+    int entry, clear;
 };
 constexpr int PER_THREAD = 2;  // sequences of a thread at most: no more than tiles, which are 512 at most
 
@@ -185,7 +188,7 @@ __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, con
         int tiles, steps;
         size(0, tiles, steps);
         const int parts = min(max(steps / share_of((long long)tiles * steps), 1), plan.most);
-        return {x < (long long)tiles * parts ? 0 : -1, x % parts, parts, x / parts, x, -1};
+        return {x < (long long)tiles * parts ? 0 : -1, x % parts, parts, x / parts, x, -1, -1};
     }
     const int r0 = min((int)threadIdx.x * chunk, c.n_seq);
     int tiles[PER_THREAD], steps[PER_THREAD];
@@ -221,19 +224,19 @@ __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, con
         }
     }
     __syncthreads();
-    if (x >= total) return {-1, 0, 1, 0, x, -1};
+    if (x >= total) return {-1, 0, 1, 0, x, -1, -1};
     const int parts = uniform(found_parts), rest = uniform((int)found_rest);
-    return {uniform(found_seq), rest % parts, parts, rest / parts, x, -1};
+    return {uniform(found_seq), rest % parts, parts, rest / parts, x, -1, -1};
 }
 
 // A tree's call may have many more tiles than workgroups are wanted: parts are numbered in the
-// workspace among those of split tiles alone.  (Such a tile's keys are 3/2 shares at least and its parts at
+// workspace among those of split tiles alone, and so are these.  (Such a tile's keys are 3/2 shares at least and its parts at
 // most 4/3 as many as shares: 4/3 groups in all, of the 2 groups that there are.)
 template <int NW>
 __device__ __forceinline__ Part find_part_tree(const KvDev &c, const AttnArgs &a, const Plan &plan, int x, int rows, int keys)
 {
     __shared__ u64 sums[2][NW], found;
-    __shared__ int found_seq, found_rest;
+    __shared__ int found_seq, found_rest, found_parts;
     const int G = a.heads / c.kvh, chunk = (c.n_seq + NW * SAE_WAVE - 1) / (NW * SAE_WAVE);
     const int lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
     // tiles of sequence r, and their steps
@@ -254,7 +257,8 @@ __device__ __forceinline__ Part find_part_tree(const KvDev &c, const AttnArgs &a
         size(0, tiles, steps);
         const int parts = parts_of((u64)tiles * steps, steps), sub = (int)((uint32_t)x / (uint32_t)parts);
         const bool held = sub < tiles && parts > 1;
-        return {sub < tiles ? 0 : -1, x - sub * parts, parts, sub, held ? x : -1, held ? -1 : x};
+        return {sub < tiles ? 0 : -1, x - sub * parts, parts, sub, held ? x : -1, held && x == sub * parts ? sub : -1,
+                x >= (parts > 1 ? tiles : 0) ? x : -1};
     }
     const int r0 = min((int)threadIdx.x * chunk, c.n_seq);
     int tiles[PER_THREAD], steps[PER_THREAD];
@@ -273,13 +277,13 @@ __device__ __forceinline__ Part find_part_tree(const KvDev &c, const AttnArgs &a
     u64 total = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) total += sums[0][w];
-    // workgroups (upper word) and places in the workspace
+    // three sums in one: workgroups (24 bits), split tiles (20), their parts (20)
+    auto packed = [](u64 tiles, u64 parts) { return tiles * parts << 40 | (parts > 1 ? tiles << 20 | tiles * parts : 0); };
     u64 count = 0;
 #pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
         steps[i] = parts_of(total, steps[i]);  // parts from here on
-        const u64 k = (u64)tiles[i] * steps[i];
-        count += k << 32 | (steps[i] > 1 ? k : 0);
+        count += packed(tiles[i], steps[i]);
     }
     const u64 upto_here = sum_upto(count);
     if (lane == SAE_WAVE - 1) sums[1][wave] = upto_here;
@@ -292,20 +296,22 @@ __device__ __forceinline__ Part find_part_tree(const KvDev &c, const AttnArgs &a
     }
 #pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
-        const u64 k = (u64)tiles[i] * steps[i];
-        const int rest = x - (int)(before >> 32);
-        if (rest >= 0 && rest < (int)k) {  // one thread
+        const int rest = x - (int)(before >> 40);
+        if (rest >= 0 && rest < tiles[i] * steps[i]) {  // one thread
             found_seq = r0 + i;
             found_rest = rest;
-            found = (u64)(uint32_t)steps[i] << 32 | (steps[i] > 1 ? (uint32_t)before + (uint32_t)rest : ~0u);
+            found_parts = steps[i];
+            found = before;
         }
-        before += k << 32 | (steps[i] > 1 ? k : 0);
+        before += packed(tiles[i], steps[i]);
     }
     __syncthreads();
-    const int clear = x >= (int)(uint32_t)all ? x : -1;
-    if (x >= (int)(all >> 32)) return {-1, 0, 1, 0, -1, clear};
-    const int parts = uniform((int)(found >> 32)), rest = uniform(found_rest), sub = (int)((uint32_t)rest / (uint32_t)parts);
-    return {uniform(found_seq), rest - sub * parts, parts, sub, uniform((int)(uint32_t)found), clear};
+    const int clear = x >= (int)(all >> 20 & 0xFFFFF) ? x : -1;
+    if (x >= (int)(all >> 40)) return {-1, 0, 1, 0, -1, -1, clear};
+    const int parts = uniform(found_parts), rest = uniform(found_rest), sub = (int)((uint32_t)rest / (uint32_t)parts);
+    const u64 at = (u64)uniform((long long)found);
+    return {uniform(found_seq), rest - sub * parts, parts, sub, parts > 1 ? (int)(at & 0xFFFFF) + rest : -1,
+            parts > 1 && rest == sub * parts ? (int)(at >> 20 & 0xFFFFF) + sub : -1, clear};
 }
 
 // A split tile as the workspace has it, by the workgroup of its first part.
@@ -313,6 +319,17 @@ struct Split {
     int token, head0, rows;  // token: row of the call's arrays of its first token
     int parts;               // in workgroups x .. x + parts - 1; < 2: none
 };
+
+// What a workgroup of a tree's call notes of its part for the join.
+__device__ __forceinline__ void note_split(const AttnArgs &a, const Plan &plan, const Part &p, const Tile &t, int kvhead)
+{
+    if (kvhead != 0 || threadIdx.x != 0) return;
+    Split *const at = static_cast<Split *>(a.work);  // {token, head0 | rows << 16, place of the first part, parts}
+    // (no place is written past the last)
+    if (p.clear >= 0 && p.clear < plan.joins) at[p.clear] = Split{0, 0, 0, 0};
+    if (p.entry >= 0 && p.entry < plan.joins)
+        at[p.entry] = Split{t.first + t.token0, t.head0 | t.rows << 16, p.slot, p.slot + p.parts <= plan.slots ? p.parts : 0};
+}
 
 // A step's keys or values on their way from the cache to LDS: 16-byte pieces of
 // a thread, unit i of the wave's 1 KiB units.
@@ -646,14 +663,7 @@ k_prefill(KvDev c, AttnArgs a, Plan plan)
         if (p.seq >= 0) t = tile_of<TREE>(c, a, p.seq, p.sub, NW * ROWS, KEYS);
         slot = p.slot;
         if constexpr (TREE) {
-            if (kvhead == 0 && threadIdx.x == 0) {
-                // (not with a q_start that decreases; no place is written past the last)
-                if (p.clear >= 0 && p.clear < plan.slots) static_cast<Split *>(a.work)[p.clear] = Split{0, 0, 0, 0};
-                if (p.slot >= 0 && p.slot < plan.slots)
-                    static_cast<Split *>(a.work)[p.slot] = p.part == 0 && p.slot + p.parts <= plan.slots
-                                                               ? Split{t.first + t.token0, t.head0, t.rows, p.parts}
-                                                               : Split{0, 0, 0, 0};
-            }
+            note_split(a, plan, p, t, kvhead);
         } else if (kvhead == 0 && threadIdx.x == 0)
             // (parts past the grid: only with a q_start that decreases)
             static_cast<Split *>(a.work)[x] = p.seq >= 0 && p.part == 0 && x + p.parts <= plan.groups + plan.tiles
@@ -1179,6 +1189,72 @@ __global__ void __launch_bounds__(NW * SAE_WAVE) k_prefill_join(KvDev c, AttnArg
 // for sixteen ragged ones.
 constexpr int WAVES = 4;
 
+// Adds a split tile's parts for a tree's call: a workgroup 32 dimensions of 32 rows, wave w parts
+// w, w + 4, ..., four of them in flight.  (A wave for each 32 rows, one part after the other, as
+// k_prefill_join: 14.7 us where 64 rows of each tile lie in 8 parts, 8.6 in 2 of 3.)
+template <int TYPE, int D>
+__global__ void __launch_bounds__(4 * SAE_WAVE) k_tree_join(KvDev c, AttnArgs a, Plan plan)
+{
+    constexpr int NW = 4, UN = 4;
+    constexpr bool F16 = is_f16(TYPE);
+    __shared__ f32x4 os[NW][4][SAE_WAVE];
+    __shared__ float2 mls[NW][SAE_WAVE];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / SAE_WAVE), b = blockIdx.y, tile = blockIdx.z;
+    const int kvhead = blockIdx.x % c.kvh, G = a.heads / c.kvh;
+    const Split t = static_cast<const Split *>(a.work)[blockIdx.x / c.kvh];
+    const int head0 = t.head0 & 0xFFFF, rows = t.head0 >> 16, slot = t.rows;
+    if (t.parts < 2 || tile * ROWS >= rows) return;
+    const int lane = (int)__lane_id(), n = lane & 31, h = lane >> 5;
+    const int row = tile * ROWS + n;
+    const float *from = parts_of(a, plan) + part_at<D, WAVES>(c, slot, kvhead, tile);
+    const int64_t stride = c.kvh * WAVES * part_floats(D);
+    float m = NEG_INF, l = 0.0f;
+    f32x4 o[4] = {};
+    for (int p = wave; p < t.parts; p += NW * UN) {
+        float2 ml[UN];
+        f32x4 y[UN][4];
+#pragma unroll
+        for (int k = 0; k < UN; ++k) {
+            const float *at = from + min(p + k * NW, t.parts - 1) * stride;  // past the end: not added below
+            ml[k] = *reinterpret_cast<const float2 *>(at + ROWS * D + lane * 2);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[k][e] = *reinterpret_cast<const f32x4 *>(at + (b * 4 + e) * 256 + lane * 4);
+        }
+#pragma unroll
+        for (int k = 0; k < UN; ++k) {
+            if (p + k * NW >= t.parts) break;  // uniform
+            const float top = fmaxf(m, ml[k].x), mu = top == NEG_INF ? 0.0f : top;
+            const float f0 = exp2_(m - mu), f1 = exp2_(ml[k].x - mu);
+            l = l * f0 + ml[k].y * f1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = o[e] * f0 + y[k][e] * f1;
+            m = top;
+        }
+    }
+    mls[wave][lane] = float2{m, l};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) os[wave][e][lane] = o[e];
+    __syncthreads();
+    float top = NEG_INF, z = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, mls[w][lane].x);
+    const float mu = top == NEG_INF ? 0.0f : top;
+    f32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const float f = exp2_(mls[w][lane].x - mu);
+        z += mls[w][lane].y * f;
+        sum += os[w][wave][lane] * f;
+    }
+    if (row >= rows) return;
+    const int64_t token = t.token + (head0 + row) / G, head = kvhead * G + (head0 + row) % G;
+    const float inv = z == 0.0f ? 0.0f : 1.0f / z;
+    char *to = static_cast<char *>(a.out) + (token * a.out_stride + head * D + b * 32 + wave * 8 + h * 4) * 2;
+    *reinterpret_cast<u32x2 *>(to) = u32x2{pack2<F16>(mean<F16>(sum[0] * inv), mean<F16>(sum[1] * inv)),
+                                           pack2<F16>(mean<F16>(sum[2] * inv), mean<F16>(sum[3] * inv))};
+    if (a.lse && wave == 0 && h == 0 && b == 0) a.lse[token * a.heads + head] = z == 0.0f ? NEG_INF : (top + log2_(z)) * LN2;
+}
+
 int64_t tiles_of(const KvDev &c, int heads)
 {
     const int64_t G = heads / c.kvh, rows = WAVES * ROWS;
@@ -1191,7 +1267,7 @@ int64_t tiles_of(const KvDev &c, int heads)
 // same keys spread evenly 162.
 Plan plan_of(const KvDev &c, int heads, int dim, int window, int nodes)
 {
-    Plan p = {(int)tiles_of(c, heads), 0, 1, 0};
+    Plan p = {(int)tiles_of(c, heads), 0, 1, 0, 0};
     // no tile has more parts than MIN_SPLIT goes into the keys that it can see
     int64_t keys = (int64_t)c.max_blocks * SAE_KV_BLOCK;
     if (window > 0) keys = std::min(keys, (int64_t)window + WAVES * ROWS + nodes + keys_of(dim));
@@ -1200,8 +1276,18 @@ Plan plan_of(const KvDev &c, int heads, int dim, int window, int nodes)
     if ((few || nodes > 0) && c.n_seq <= PER_THREAD * WAVES * SAE_WAVE && keys > SHORT) {
         p.groups = std::max(groups_of(dim) / c.kvh, 1);
         p.slots = few ? p.groups + p.tiles : 2 * p.groups;
+        p.joins = std::min(p.tiles, 2 * p.groups / 3 + 1);  // (each has two parts, of 3/4 of a share at least)
     }
     return p;
+}
+
+template <int TYPE, int D>
+hipError_t launch_tree_join(const KvDev &c, const AttnArgs &a, const Plan &p, hipStream_t s)
+{
+    const int64_t rows = std::min((int64_t)a.max_nodes * (a.heads / c.kvh), (int64_t)WAVES * ROWS);  // of a tile at most
+    hipLaunchKernelGGL((k_tree_join<TYPE, D>), dim3((unsigned)(p.joins * c.kvh), D / 32, (unsigned)((rows + ROWS - 1) / ROWS)),
+                       dim3(4 * SAE_WAVE), 0, s, c, a, p);
+    return hipGetLastError();
 }
 
 template <int TYPE, int D, bool TREE>
@@ -1213,11 +1299,12 @@ hipError_t launch(const KvDev &c, const AttnArgs &a, hipStream_t s)
         return hipGetLastError();
     }
     // parts: at most a share of the work each, rounded up for every tile
-    const unsigned grid = (unsigned)((p.groups + p.tiles) * c.kvh), joins = (unsigned)(p.slots * c.kvh);
+    const unsigned grid = (unsigned)((p.groups + p.tiles) * c.kvh);
     hipLaunchKernelGGL((k_prefill<TYPE, D, WAVES, true, TREE>), dim3(grid), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_prefill_join<TYPE, D, WAVES>), dim3(joins, D / 32), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
+    if constexpr (TREE) return launch_tree_join<TYPE, D>(c, a, p, s);
+    hipLaunchKernelGGL((k_prefill_join<TYPE, D, WAVES>), dim3(grid, D / 32), dim3(WAVES * SAE_WAVE), 0, s, c, a, p);
     return hipGetLastError();
 }
 
