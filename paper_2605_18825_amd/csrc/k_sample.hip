@@ -17,6 +17,17 @@
 //   2.2 % of weight wide, and what it leaves open of one answer leaves the next one a bin or two.
 //   where these are more than LDS holds, each question is answered by itself: its bin, then
 //   (a bin of many equal or near logits) 10 bits of the logit at a time, then the index.
+//
+// Bound by the logits' bytes with a small k: 256 rows of 131,072 bf16 logits 20.7 us, 3.2 TB/s with a
+// few dependent steps behind it.  Otherwise by the histogram's pass, in vector instructions: for a row
+// of 100,003 f32 logits it takes 57 thousand clocks, 26 thousand without the weights.  64 rows of 100,003 with
+// nothing left out: 46.8 us; 700 rows of 50,001 with settings of their own: 75.6.
+//
+// Few rows of a large vocabulary leave most of the GPU idle: there the first two passes are launches
+// of their own, a row's vectors over several workgroups, maxima and the histogram in the workspace (whole
+// numbers added by atomics: in any order the same), and the rest is as above.
+#include <algorithm>
+
 #include "attn_tile.h"
 
 namespace {
@@ -43,6 +54,16 @@ struct Args {
     int32_t *token, *kept;
     float *prob;
     int32_t vocab;
+    char *work;
+};
+
+// A row's part of the workspace, where its passes are launches of their own.
+constexpr int SPLIT_GROUPS = GROUPS * 1024, SPLIT_MAXES = 64;
+struct Shelf {
+    u64 mass[BINS];
+    uint32_t count[BINS];
+    float most[SPLIT_GROUPS];  // maxima of vectors i SPLIT_GROUPS + g, for each g
+    float maxes[SPLIT_MAXES];  // the workgroups' maxima
 };
 
 // ------------------------------------------------------------- waves and workgroups
@@ -139,16 +160,34 @@ struct Row {
     }
     __device__ __forceinline__ u32x4 vector(int v) const { return *reinterpret_cast<const u32x4 *>(body + (int64_t)v * 16); }
 
-    // The first pass: the thread's maxima; returns the largest.
-    __device__ __forceinline__ float maxima()
+    __device__ __forceinline__ void load_edge()
     {
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) most[g] = LOWEST;
         edge = LOWEST;
         if (edge_at >= 0) {
             if constexpr (DT == SAE_ROWS_F32) edge = fmaxf(reinterpret_cast<const float *>(at)[edge_at], LOWEST);
             else edge = fmaxf(attn::low<DT == SAE_KV_F16>((uint32_t)reinterpret_cast<const uint16_t *>(at)[edge_at]), LOWEST);
         }
+    }
+    // The maxima that the first launch has left; returns the thread's largest.
+    __device__ __forceinline__ float maxima_of(const Shelf &shelf)
+    {
+        static_assert(GROUPS * THREADS == SPLIT_GROUPS || THREADS != 1024, "a thread has groups t, t + THREADS, ...");
+        load_edge();
+        float m = edge;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            const int v = g * THREADS + (int)threadIdx.x;
+            most[g] = v < vectors ? shelf.most[v] : LOWEST;
+            m = fmaxf(m, most[g]);
+        }
+        return m;
+    }
+    // The first pass: the thread's maxima; returns the largest.
+    __device__ __forceinline__ float maxima()
+    {
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) most[g] = LOWEST;
+        load_edge();
 #pragma unroll 1
         for (int v0 = 0; v0 < vectors; v0 += GROUPS * THREADS) {
 #pragma unroll
@@ -189,14 +228,21 @@ struct Row {
     template <typename F, typename L>
     __device__ __forceinline__ void each(float bound, F f, L low) const
     {
+        each_of(0, vectors, bound, f, low);
+        if (edge_at >= 0) f(edge, edge_at);
+    }
+    // The same for vectors first .. last - 1.
+    template <typename F, typename L>
+    __device__ __forceinline__ void each_of(int first, int last, float bound, F f, L low) const
+    {
 #pragma unroll 1
-        for (int v = threadIdx.x; v < vectors; v += THREADS * UN) {
+        for (int v = first + (int)threadIdx.x; v < last; v += THREADS * UN) {
             u32x4 x[UN];
 #pragma unroll
-            for (int k = 0; k < UN; ++k) x[k] = vector(min(v + k * THREADS, vectors - 1));
+            for (int k = 0; k < UN; ++k) x[k] = vector(min(v + k * THREADS, last - 1));
 #pragma unroll
             for (int k = 0; k < UN; ++k)
-                if (v + k * THREADS < vectors) {
+                if (v + k * THREADS < last) {
                     if (bound > LOWEST && !infinite) {  // uniform
                         float m = wide(x[k], 0);
 #pragma unroll
@@ -210,7 +256,6 @@ struct Row {
                     use(x[k], v + k * THREADS, f);
                 }
         }
-        if (edge_at >= 0) f(edge, edge_at);
     }
     // Appends the indexes of all logits with pred(logit) to `list`, at most `room`; n: counts them (all).
     // Bits for four vectors at a time: a test has no branch, and a thread with any takes one place for all of them.
@@ -709,24 +754,122 @@ __device__ __forceinline__ bool answer_in_bins(Shared &s, const Row<DT, THREADS>
     return true;
 }
 
-template <int DT, int THREADS>
+struct Settings {
+    float T, p, m, u;
+    int k;
+    __device__ __forceinline__ Settings(const Args &a, int r)
+        : T(a.temperature ? a.temperature[r] : 1.0f), p(a.top_p ? a.top_p[r] : 1.0f), m(a.min_p ? a.min_p[r] : 0.0f), u(a.u[r]),
+          k(a.top_k ? a.top_k[r] : 0)
+    {
+    }
+    __device__ __forceinline__ bool greedy() const { return !(T > 0.0f) || k == 1 || p <= 0.0f; }
+};
+template <int THREADS>
+constexpr int SMALL_K = THREADS / 4;  // a k that the threads' maxima bound
+
+__device__ __forceinline__ Scale scale_of_row(float top, float T, const double *power)
+{
+    return {(double)top, PER_TWO * 1.44269504088896340736 / (double)T, power};
+}
+__device__ __forceinline__ void fill_powers(Shared &s)
+{
+    if (threadIdx.x < PER_TWO) s.power[threadIdx.x] = __builtin_ldexp(exp2(threadIdx.x * (-1.0 / PER_TWO)), 43);
+}
+
+// The first launch of few rows: maxima of the row's groups, 256 a workgroup, and an empty histogram.
+template <int DT>
+__global__ void __launch_bounds__(256) k_sample_max(Args a)
+{
+    __shared__ float part[4];
+    const int r = blockIdx.y;
+    const Row<DT, 256> row(static_cast<const char *>(a.logits) + (int64_t)r * a.stride * Row<DT, 256>::SIZE, a.vocab);
+    Shelf &shelf = reinterpret_cast<Shelf *>(a.work)[r];
+    const int g = blockIdx.x * 256 + threadIdx.x;
+    for (int i = g; i < BINS; i += gridDim.x * 256) {
+        shelf.mass[i] = 0;
+        shelf.count[i] = 0;
+    }
+    float m = LOWEST;
+    for (int v = g; v < row.vectors; v += SPLIT_GROUPS) {
+        const u32x4 x = row.vector(v);
+#pragma unroll
+        for (int i = 0; i < Row<DT, 256>::E; ++i) m = fmaxf(m, row.wide(x, i));
+    }
+    if (g < SPLIT_GROUPS) shelf.most[g] = m;
+    m = upto(m, LOWEST, [](float x, float y) { return fmaxf(x, y); });
+    if (__lane_id() == SAE_WAVE - 1) part[threadIdx.x / SAE_WAVE] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) shelf.maxes[blockIdx.x] = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+}
+
+// The second: a part of the row's vectors into the histogram.
+template <int DT>
+__global__ void __launch_bounds__(512) k_sample_hist(Args a, int maxes)
+{
+    __shared__ Shared s;
+    const int r = blockIdx.y;
+    const Settings set(a, r);
+    if (set.greedy()) return;  // uniform: not asked for
+    Row<DT, 512> row(static_cast<const char *>(a.logits) + (int64_t)r * a.stride * Row<DT, 512>::SIZE, a.vocab);
+    Shelf &shelf = reinterpret_cast<Shelf *>(a.work)[r];
+    fill_powers(s);
+    for (int i = threadIdx.x; i < BINS; i += 512) {
+        s.bins.mass[i] = 0;
+        s.bins.count[i] = 0;
+    }
+    row.load_edge();
+    const float mine = (int)threadIdx.x < maxes ? fmaxf(shelf.maxes[threadIdx.x], row.edge) : row.edge;
+    const float top = over_all<8>(s, 0, mine, LOWEST, [](float x, float y) { return fmaxf(x, y); });
+    if (!(top > LOWEST)) return;
+    if (top == __builtin_inff()) {
+        row.infinite = true;
+        row.edge = row.mapped(row.edge);
+    }
+    const Scale sc = scale_of_row(row.infinite ? 0.0f : top, set.T, s.power);
+    uint32_t light = 0;
+    auto put = [&](float l, int) {
+        double rest;
+        const int b = sc.split(l, rest);
+        if (b < LIGHT) {
+            atomicAdd(&s.bins.count[b], 1u);
+            atomicAdd(&s.bins.mass[b], sc.weight(b, rest));
+        } else {
+            light += l > LOWEST;
+        }
+    };
+    const int per = (row.vectors + (int)gridDim.x - 1) / (int)gridDim.x, first = min((int)blockIdx.x * per, row.vectors);
+    row.each_of(first, min(first + per, row.vectors), sc.floor_of(LIGHT), put, [&](float l) { light += l > LOWEST; });
+    if (blockIdx.x == 0 && row.edge_at >= 0) put(row.edge, row.edge_at);
+    light = sum_upto(light);
+    if (__lane_id() == SAE_WAVE - 1 && light) atomicAdd(&s.bins.count[LIGHT], light);
+    __syncthreads();
+    for (int i = threadIdx.x; i < BINS; i += 512)
+        if (s.bins.count[i]) {
+            atomicAdd(&shelf.count[i], s.bins.count[i]);
+            if (s.bins.mass[i]) atomicAdd(&shelf.mass[i], s.bins.mass[i]);
+        }
+}
+
+template <int DT, int THREADS, bool SPLIT>
 __global__ void __launch_bounds__(THREADS) k_sample(Args a)
 {
     constexpr int NW = THREADS / SAE_WAVE;
     __shared__ Shared s;
     const int r = blockIdx.x, lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
     Row<DT, THREADS> row(static_cast<const char *>(a.logits) + (int64_t)r * a.stride * Row<DT, THREADS>::SIZE, a.vocab);
-    const float T = a.temperature ? a.temperature[r] : 1.0f, p = a.top_p ? a.top_p[r] : 1.0f, m = a.min_p ? a.min_p[r] : 0.0f;
-    const int k = a.top_k ? a.top_k[r] : 0;
-    const float u = a.u[r];
+    const Settings set(a, r);
+    const float p = set.p, m = set.m, u = set.u;
+    const int k = SPLIT ? 0 : set.k;  // (rows with a top_k are not split)
     auto answer = [&](uint32_t token, float prob, uint32_t kept) {
         a.token[r] = (int32_t)token;
         if (a.prob) a.prob[r] = prob;
         if (a.kept) a.kept[r] = (int32_t)kept;
     };
-    if (threadIdx.x < PER_TWO) s.power[threadIdx.x] = __builtin_ldexp(exp2(threadIdx.x * (-1.0 / PER_TWO)), 43);
-
-    float mine = row.maxima();
+    const Shelf *const shelf = SPLIT ? reinterpret_cast<const Shelf *>(a.work) + r : nullptr;
+    fill_powers(s);
+    float mine;
+    if constexpr (SPLIT) mine = row.maxima_of(*shelf);
+    else mine = row.maxima();
     float top = over_all<NW>(s, 0, mine, LOWEST, [](float x, float y) { return fmaxf(x, y); });
     if (!(top > LOWEST)) {
         if (threadIdx.x == 0) answer(~0u, 0.0f, 0);
@@ -737,7 +880,7 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
         mine = row.mapped(mine);
         top = 0.0f;
     }
-    if (!(T > 0.0f) || k == 1 || p <= 0.0f) {  // the first of the largest
+    if (set.greedy()) {  // the first of the largest
         uint32_t first = ~0u;
         row.some(top, [&](float l, int i) {
             if (l == top) first = min(first, (uint32_t)i);
@@ -746,13 +889,13 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
         if (threadIdx.x == 0) answer(first, 1.0f, 1);
         return;
     }
-    const Scale sc = {(double)top, PER_TWO * 1.44269504088896340736 / (double)T, s.power};
+    const Scale sc = scale_of_row(top, set.T, s.power);
 
     // the list: the first tokens of the order, enough of them for every question
     int n = LIST + 1;    // in the list; more than LIST: not collected
     bool whole = false;  // `total` is the weight of all tokens, and top-k leaves them all
     u64 total = 0;
-    if (k > 0 && k <= THREADS / 4) {
+    if (!SPLIT && k > 0 && k <= SMALL_K<THREADS>) {
         // the k-th largest of the threads' maxima, to 16 bits of its key
         uint32_t bound = 0, want = (uint32_t)k;
         const uint32_t key = key_of(mine);
@@ -798,24 +941,25 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
     if (n > LIST) {
         __syncthreads();
         for (int i = threadIdx.x; i < BINS; i += THREADS) {
-            s.bins.mass[i] = 0;
-            s.bins.count[i] = 0;
+            s.bins.mass[i] = SPLIT ? shelf->mass[i] : 0;
+            s.bins.count[i] = SPLIT ? shelf->count[i] : 0;
         }
         if (threadIdx.x == 0) s.n = 0;
         __syncthreads();
         uint32_t light = 0;
-        row.each(row.any_below(sc.floor_of(LIGHT)),
-                 [&](float l, int) {
-                     double rest;
-                     const int b = sc.split(l, rest);
-                     if (b < LIGHT) {
-                         atomicAdd(&s.bins.count[b], 1u);
-                         atomicAdd(&s.bins.mass[b], sc.weight(b, rest));
-                     } else {
-                         light += l > LOWEST;
-                     }
-                 },
-                 [&](float l) { light += l > LOWEST; });
+        if constexpr (!SPLIT)
+            row.each(row.any_below(sc.floor_of(LIGHT)),
+                     [&](float l, int) {
+                         double rest;
+                         const int b = sc.split(l, rest);
+                         if (b < LIGHT) {
+                             atomicAdd(&s.bins.count[b], 1u);
+                             atomicAdd(&s.bins.mass[b], sc.weight(b, rest));
+                         } else {
+                             light += l > LOWEST;
+                         }
+                     },
+                     [&](float l) { light += l > LOWEST; });
         light = sum_upto(light);
         if (lane == SAE_WAVE - 1 && light) atomicAdd(&s.bins.count[LIGHT], light);
         __syncthreads();
@@ -922,22 +1066,34 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
     }
 }
 
+// Rows whose passes are launches of their own: from 65,536 tokens and to 64 rows (one row of 131,072 bf16 logits
+// with top-p: 47.0 us as one launch, 26.4 as three; 64 rows 70.9 and 58.1; 64 rows of 64,000 43.7 and 43.4, 200
+// rows of 131,072 81.5 and 94.1), but not with a top_k: rows with a small k read theirs once (14.6 us instead of 10.3).
+bool is_split(int rows, int vocab) { return vocab >= 65536 && rows <= 64; }
+
 template <int DT>
 void launch(const Args &a, int rows, hipStream_t s)
 {
-    if (a.vocab <= 8192) hipLaunchKernelGGL((k_sample<DT, 256>), dim3(rows), dim3(256), 0, s, a);
-    else if (rows >= 512) hipLaunchKernelGGL((k_sample<DT, 512>), dim3(rows), dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((k_sample<DT, 1024>), dim3(rows), dim3(1024), 0, s, a);
+    if (is_split(rows, a.vocab) && !a.top_k) {
+        const int vectors = a.vocab / Row<DT, 256>::E, maxes = std::min((vectors + 255) / 256, SPLIT_MAXES);
+        hipLaunchKernelGGL((k_sample_max<DT>), dim3(maxes, rows), dim3(256), 0, s, a);
+        // about two workgroups per compute unit, of at least 4 vectors a thread
+        const int parts = std::max(std::min(512 / rows, vectors / 2048), 1);
+        hipLaunchKernelGGL((k_sample_hist<DT>), dim3(parts, rows), dim3(512), 0, s, a, maxes);
+        hipLaunchKernelGGL((k_sample<DT, 1024, true>), dim3(rows), dim3(1024), 0, s, a);
+    } else if (a.vocab <= 8192) hipLaunchKernelGGL((k_sample<DT, 256, false>), dim3(rows), dim3(256), 0, s, a);
+    else if (rows >= 512) hipLaunchKernelGGL((k_sample<DT, 512, false>), dim3(rows), dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_sample<DT, 1024, false>), dim3(rows), dim3(1024), 0, s, a);
 }
 
 }  // namespace
 
-size_t sample_work_bytes(int, int) { return 16; }
+size_t sample_work_bytes(int rows, int vocab) { return rows > 0 && is_split(rows, vocab) ? rows * sizeof(Shelf) : 16; }
 
 hipError_t launch_sample(int rows, int vocab, int dtype, const SampleArgs &x, hipStream_t s)
 {
     const Args a = {x.logits, x.stride, x.settings.temperature, x.settings.top_p, x.settings.min_p, x.u, x.settings.top_k,
-                    x.token, x.kept, x.prob, vocab};
+                    x.token, x.kept, x.prob, vocab, static_cast<char *>(x.work)};
     if (dtype == SAE_KV_BF16) launch<SAE_KV_BF16>(a, rows, s);
     else if (dtype == SAE_KV_F16) launch<SAE_KV_F16>(a, rows, s);
     else launch<SAE_ROWS_F32>(a, rows, s);

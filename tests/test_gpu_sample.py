@@ -228,3 +228,88 @@ def test_graph_replays_with_new_rows():
         step(eager)
         torch.cuda.synchronize()
         assert torch.equal(token, eager)
+
+
+SPLIT_MIXES = {
+    "whole": {}, "temperature": dict(temperature=[0.2, 0.0, 1.0, 3.0]), "top_p": dict(top_p=[0.1, 0.5, 0.9, 0.99]),
+    "min_p": dict(min_p=[0.001, 0.05, 0.5, 1.0]),
+    "all": dict(temperature=[0.8, 1.2, 0.5, 2.0], top_p=[0.95, 0.0, 1.0, 0.7], min_p=[0.01, 0.1, 0.0, 0.2]),
+}
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("mix", sorted(SPLIT_MIXES))
+@pytest.mark.parametrize("n,vocab", [(1, 65536), (5, 65537), (3, 100003), (2, 262144)])
+def test_rows_that_several_workgroups_read(dtype, mix, n, vocab):
+    """Few rows of a large vocabulary without a top_k; at odd sizes no row but the first is aligned."""
+    x, u = logits(n, vocab, dtype, seed=vocab)
+    check(x, u, **spread_over(n, SPLIT_MIXES[mix]))
+
+
+def test_split_rows_either_side_of_the_rule():
+    """The same answers of rows that are split, of more rows, which are not, and with a top_k that leaves all."""
+    x, u = logits(65, 65600, "bf16", seed=21, spread=1.5)
+    p = [0.5 + 0.007 * r for r in range(65)]
+    many = call(x.cuda(), u, top_p=p)
+    few = [call(x[a:b].cuda(), u[a:b], top_p=p[a:b]) for a, b in ((0, 1), (1, 65))]
+    all_k = call(x[1:].cuda(), u[1:], top_p=p[1:], top_k=[65600] * 64)
+    for i in range(3):
+        assert np.array_equal(many[i], np.concatenate([f[i] for f in few]))
+        assert np.array_equal(many[i][1:], all_k[i])
+
+
+def test_split_rows_that_nothing_is_left_of():
+    vocab = 70001
+    x, u = logits(7, vocab, "f32", seed=22)
+    x[0] = -np.inf
+    x[1] = np.nan
+    x[2, 1:] = -np.inf
+    x[3, ::2] = np.nan
+    x[4, :-1] = -np.inf
+    x[5, [7, 40000, vocab - 1]] = np.inf
+    x[6] = 0.5
+    for settings in ({}, dict(top_p=[0.9] * 7), dict(temperature=[0.0] * 7), dict(top_p=[0.7] * 7, min_p=[0.1] * 7)):
+        token, prob, kept = check(x, u, **settings)
+        assert np.all(token[:2] == -1) and np.all(kept[:2] == 0) and np.all(prob[:2] == 0)
+        assert token[2] == 0 and token[4] == vocab - 1 and prob[4] == 1 and kept[4] == 1
+
+
+def test_split_rows_apart_and_out_of_line():
+    n, vocab = 3, 65541
+    x, u = logits(n, vocab, "bf16", seed=23)
+    for lead, width in ((1, vocab + 4), (3, vocab + 8), (7, vocab + 16)):
+        wide = torch.full((n * width + 16,), float("inf"), dtype=torch.bfloat16, device="cuda")
+        view = wide[lead:lead + n * width].view(n, width)[:, :vocab]
+        view.copy_(x)
+        check(view, u, top_p=[0.9] * n)
+
+
+def test_split_rows_in_a_graph():
+    """The histogram in the workspace begins anew in each replay, and in eager calls between them."""
+    n, vocab = 4, 90001
+    x, u = torch.empty((n, vocab), device="cuda"), torch.empty(n, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    token, eager = (torch.empty(n, dtype=torch.int32, device="cuda") for _ in range(2))
+    work = torch.full((api.sae_sample_work_size(n, vocab),), 0xFF, dtype=torch.uint8, device="cuda")
+    p = torch.tensor([0.9, 1.0, 0.5, 0.99], device="cuda")
+
+    def step(to):
+        api.sae_sample(x, u, to, work, top_p=p)
+    x.normal_(generator=g)
+    u.uniform_(generator=g)
+    step(eager)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(token)
+    for i in range(6):
+        x.normal_(generator=g).mul_(1 + i)
+        u.uniform_(generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        step(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(token, eager)
+        for r in range(n):
+            assert int(token[r]) == S.sample(x[r].double().cpu().numpy(), float(u[r]), top_p=float(p[r]))[0]
