@@ -114,11 +114,11 @@ enum {
     SAE_ST_SLOT_BUSY = 1u << 4,       /* insert into a valid slot (insert skipped)   */
     SAE_ST_SELECT_FALLBACK = 1u << 5, /* exact slow path of the pool scan was used   */
     SAE_ST_BAD_BLOCK = 1u << 6,       /* block id out of range (element skipped)     */
-    SAE_ST_BAD_TREE = 1u << 8,        /* sae_attn_tree: a parent that is not an earlier
-                                         token, or too many tokens                  */
-    SAE_ST_BAD_HASH = 1u << 7         /* a reserved hash (0 or 2^64-1) given to Add()
+    SAE_ST_BAD_HASH = 1u << 7,        /* a reserved hash (0 or 2^64-1) given to Add()
                                          or found in a valid block by the index build:
                                          that block is skipped (not added, not indexed) */
+    SAE_ST_BAD_TREE = 1u << 8         /* sae_attn_tree: a parent that is not an earlier
+                                         token, or too many tokens                  */
 };
 
 typedef struct {
@@ -539,7 +539,8 @@ sae_status sae_predict_sessions_noalloc(int32_t n, int32_t d, const uint16_t *h,
  *                16 * n_kv_heads
  *  status        device uint32 or NULL: SAE_ST_BAD_BLOCK is ORed into it where a
  *                table holds a block id >= blocks_per_instance, an instance out of
- *                range, or a length outside 0 .. 16 max_blocks
+ *                range, or a length outside 0 .. 16 max_blocks; SAE_ST_BAD_TREE
+ *                by sae_attn_tree
  * Place of token t, dimension d in a page, with c = 16 bytes / value size:
  *  keys    [D / c][16][c]               at [d / c][t][d % c]
  *  values  [D / 2c][16][2][c / 8][2][4] at [d / 2c][d % 16][t / 4 % 2]

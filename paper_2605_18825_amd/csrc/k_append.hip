@@ -199,10 +199,9 @@ __global__ void __launch_bounds__(THREADS, 4) k_kv_append(KvDev c, Append a)
     const Place p = place_of(c, blockIdx.x);
     const int start = blockIdx.y * THREADS + threadIdx.x, step = gridDim.y * THREADS;
     if (a.q_out)  // rows without a place
-        for (int i = start; i < (p.dead1 - p.dead0) * a.heads * (D / 8); i += step) {
-            const int row = i / (a.heads * (D / 8)), at = i % (a.heads * (D / 8));
-            *reinterpret_cast<u32x4 *>(a.q_out + (int64_t)(p.dead0 + row) * a.out_stride + at * 8) = u32x4{0, 0, 0, 0};
-        }
+        for (int row = p.dead0; row < p.dead1; ++row)
+            for (int i = start; i < a.heads * (D / 8); i += step)
+                *reinterpret_cast<u32x4 *>(a.q_out + row * a.out_stride + i * 8) = u32x4{0, 0, 0, 0};
     if (p.none) return;
     // items: [key-value heads, then query heads][token groups of the tile][lanes of a row]
     const int tg0 = p.t_lo / 4, groups = (p.t_hi + 3) / 4 - tg0;
