@@ -21,7 +21,7 @@
 // Bound by the logits' bytes with a small k: 256 rows of 131,072 bf16 logits 20.7 us, 3.2 TB/s with a
 // few dependent steps behind it.  Otherwise by the histogram's pass, in vector instructions: for a row
 // of 100,003 f32 logits it takes 57 thousand clocks, 26 thousand without the weights.  64 rows of 100,003 with
-// nothing left out: 46.8 us; 700 rows of 50,001 with settings of their own: 75.6.
+// nothing left out: 45 to 47 us by card; 700 rows of 50,001 with settings of their own: 72.5.
 //
 // Few rows of a large vocabulary leave most of the GPU idle: there the first two passes are launches
 // of their own, a row's vectors over several workgroups, maxima and the histogram in the workspace (whole
@@ -457,20 +457,46 @@ __device__ __forceinline__ void sort_and_sum(Shared &s, const Scale &sc, int n, 
     while (size < n) size *= 2;
     for (int i = n + threadIdx.x; i < size; i += THREADS) s.list[i] = ~0ull;
     __syncthreads();
+    // a bitonic network, two of its stages at a time
+    auto order = [](u64 &a, u64 &b, bool up) {
+        const bool swap = (a > b) == up;
+        const u64 x = swap ? b : a;
+        b = swap ? a : b;
+        a = x;
+    };
 #pragma unroll 1
-    for (int k = 2; k <= size; k *= 2)
-#pragma unroll 1
-        for (int j = k / 2; j > 0; j /= 2) {
+    for (int k = 2; k <= size; k *= 2) {
+        int j = k / 2;
+        if (__builtin_ctz(k) & 1) {
             for (int t = threadIdx.x; t < size / 2; t += THREADS) {
                 const int i = (t & ~(j - 1)) * 2 + (t & (j - 1));
-                const u64 a = s.list[i], b = s.list[i + j];
-                if ((a > b) == ((i & k) == 0)) {
-                    s.list[i] = b;
-                    s.list[i + j] = a;
-                }
+                u64 a = s.list[i], b = s.list[i + j];
+                order(a, b, (i & k) == 0);
+                s.list[i] = a;
+                s.list[i + j] = b;
+            }
+            __syncthreads();
+            j /= 2;
+        }
+#pragma unroll 1
+        for (; j > 0; j /= 4) {
+            const int h = j / 2;
+            for (int t = threadIdx.x; t < size / 4; t += THREADS) {
+                const int i = (t & ~(h - 1)) * 4 + (t & (h - 1));
+                const bool up = (i & k) == 0;
+                u64 a = s.list[i], b = s.list[i + h], c = s.list[i + 2 * h], d = s.list[i + 3 * h];
+                order(a, c, up);
+                order(b, d, up);
+                order(a, b, up);
+                order(c, d, up);
+                s.list[i] = a;
+                s.list[i + h] = b;
+                s.list[i + 2 * h] = c;
+                s.list[i + 3 * h] = d;
             }
             __syncthreads();
         }
+    }
     const int per = (n + THREADS - 1) / THREADS, i0 = threadIdx.x * per;
     u64 m[PER], sum = 0;
 #pragma unroll
@@ -592,7 +618,19 @@ __device__ __forceinline__ bool answer_in_bins(Shared &s, const Row<DT, THREADS>
     constexpr int NW = THREADS / SAE_WAVE;
     auto mass_of = [&](int b) { return b < 0 ? (u64)0 : uniform64(s.bins.mass[b]); };
     auto count_of = [&](int b) { return b < 0 ? 0 : uniform((int)s.bins.count[b]); };
-    auto bin_of = [&](u64 mass) { return first_of(BINS, [&](int i) { return s.bins.mass[i] >= mass; }); };
+    // the first bin that reached(mass, count) holds for; each lane keeps what is reached every 24 bins
+    constexpr int STEP = BINS / SAE_WAVE;
+    const int lane = (int)__lane_id();
+    const u64 far_mass = s.bins.mass[lane * STEP + STEP - 1];
+    const uint32_t far_count = s.bins.count[lane * STEP + STEP - 1];
+    auto first_bin = [&](auto reached) __attribute__((always_inline)) {
+        u64 in = __ballot(reached(far_mass, far_count));
+        if (!in) return BINS - 1;
+        const int from = __builtin_ctzll(in) * STEP, i = min(from + lane, BINS - 1);
+        in = __ballot(lane < STEP && reached(s.bins.mass[i], s.bins.count[i]));
+        return from + (int)__builtin_ctzll(in);
+    };
+    auto bin_of = [&](u64 mass) { return first_bin([&](u64 x, uint32_t) { return x >= mass; }); };
     int lo[4] = {-2, -2, -2, -2}, hi[4] = {-2, -2, -2, -2};  // of bins; rising and apart in the end
     auto add = [&](int question, int x, int y) __attribute__((always_inline)) {
 #pragma unroll
@@ -609,7 +647,7 @@ __device__ __forceinline__ bool answer_in_bins(Shared &s, const Row<DT, THREADS>
     u64 w0 = all, w1 = all;  // bounds of the weight that is left
     int b0 = -1;
     if (!whole) {
-        b0 = first_of(BINS, [&](int i) { return s.bins.count[i] >= kth; });
+        b0 = first_bin([&](u64, uint32_t x) { return x >= kth; });
         w0 = mass_of(b0 - 1);
         w1 = mass_of(b0);
         if (b0 < LIGHT) add(0, b0, b0);
@@ -646,16 +684,23 @@ __device__ __forceinline__ bool answer_in_bins(Shared &s, const Row<DT, THREADS>
                 lo[i + 1] = a;
                 hi[i + 1] = b;
             }
-    int at[4], n = 0;
-    u64 gap[4], held = 0;
+    int end = -1;  // lanes 2 i and 2 i + 1: the bins before and at the end of range i
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        end = lane == 2 * i ? lo[i] - 1 : end;
+        end = lane == 2 * i + 1 ? hi[i] : end;
+    }
+    const u64 end_mass = end < 0 ? 0 : s.bins.mass[end];
+    const uint32_t end_count = end < 0 ? 0 : s.bins.count[end];
+    int at[4], n = 0, behind[4];
+    u64 gap[4], held = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // (an empty range: no mass, no tokens)
         at[i] = n;
-        gap[i] = 0;
-        if (lo[i] < 0) continue;
-        gap[i] = mass_of(lo[i] - 1) - held;
-        n += count_of(hi[i]) - count_of(lo[i] - 1);
-        held += mass_of(hi[i]) - mass_of(lo[i] - 1);
+        behind[i] = (int)of_lane(end_count, 2 * i);
+        gap[i] = of_lane(end_mass, 2 * i) - held;
+        n += (int)of_lane(end_count, 2 * i + 1) - behind[i];
+        held += of_lane(end_mass, 2 * i + 1) - of_lane(end_mass, 2 * i);
     }
     if (n > LIST) return false;
     __syncthreads();
@@ -674,9 +719,12 @@ __device__ __forceinline__ bool answer_in_bins(Shared &s, const Row<DT, THREADS>
         least[j] = s.edges[2 * j];
         past[j] = s.edges[2 * j + 1];
     }
+    // (what lies between several ranges collected too and sifted in LDS, where it is little: no faster)
     uint32_t *indexes = reinterpret_cast<uint32_t *>(s.sums);
     if (lo[2] < 0)  // uniform: one range
         row.collect(indexes, &s.n, LIST, [&](float l) { return (l >= least[3]) & (l < past[3]); });
+    else if (lo[1] < 0)  // two
+        row.collect(indexes, &s.n, LIST, [&](float l) { return ((l >= least[2]) & (l < past[2])) | ((l >= least[3]) & (l < past[3])); });
     else
         row.collect(indexes, &s.n, LIST, [&](float l) {
             return ((l >= least[0]) & (l < past[0])) | ((l >= least[1]) & (l < past[1])) | ((l >= least[2]) & (l < past[2])) |
@@ -700,7 +748,7 @@ __device__ __forceinline__ bool answer_in_bins(Shared &s, const Row<DT, THREADS>
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (lo[j] >= 0 && i >= at[j]) {
-                b = count_of(lo[j] - 1);
+                b = behind[j];
                 first = at[j];
             }
         return b + i - first;
@@ -712,7 +760,7 @@ __device__ __forceinline__ bool answer_in_bins(Shared &s, const Row<DT, THREADS>
             int i = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (lo[j] >= 0 && lo[j] <= b0) i = at[j] + (int)kth - 1 - count_of(lo[j] - 1);
+                if (lo[j] >= 0 && lo[j] <= b0) i = at[j] + (int)kth - 1 - behind[j];
             w = uniform64(s.sums[i]);
         }
     }
@@ -728,8 +776,8 @@ __device__ __forceinline__ bool answer_in_bins(Shared &s, const Row<DT, THREADS>
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (lo[j] >= 0 && lo[j] <= bm && hi[j] >= bm + 2) {
-                from = at[j] + count_of(bm - 1) - count_of(lo[j] - 1);
-                to = at[j] + count_of(bm + 2) - count_of(lo[j] - 1);
+                from = at[j] + count_of(bm - 1) - behind[j];
+                to = at[j] + count_of(bm + 2) - behind[j];
             }
         __syncthreads();
         if (threadIdx.x == 0) s.found = to;
