@@ -18,7 +18,7 @@
 //   where these are more than LDS holds, each question is answered by itself: its bin, then
 //   (a bin of many equal or near logits) 10 bits of the logit at a time, then the index.
 //
-// Bound by the logits' bytes with a small k: 256 rows of 131,072 bf16 logits 20.7 us, 3.2 TB/s with a
+// Bound by the logits' bytes with a small k: 256 rows of 131,072 bf16 logits 18.6 us, 3.6 TB/s with a
 // few dependent steps behind it.  Otherwise by the histogram's pass, in vector instructions: for a row
 // of 100,003 f32 logits it takes 57 thousand clocks, 26 thousand without the weights.  64 rows of 100,003 with
 // nothing left out: 45 to 47 us by card; 700 rows of 50,001 with settings of their own: 72.5.
@@ -898,8 +898,9 @@ __global__ void __launch_bounds__(512) k_sample_hist(Args a, int maxes)
         }
 }
 
+// (Four waves a SIMD, two workgroups of 512 a compute unit: 700 rows of 50,001 at 130 registers 90 us, at 120 72.5.)
 template <int DT, int THREADS, bool SPLIT>
-__global__ void __launch_bounds__(THREADS) k_sample(Args a)
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 4) k_sample(Args a)
 {
     constexpr int NW = THREADS / SAE_WAVE;
     __shared__ Shared s;
@@ -1040,10 +1041,22 @@ __global__ void __launch_bounds__(THREADS) k_sample(Args a)
         }
     }
     if (n <= SAE_WAVE) {  // one wave, a token a lane
-        if (wave != 0) return;
+        // ranks: each wave counts what of its part of the list comes before a token
         u64 item = lane < n ? s.list[lane] : ~0ull;
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += of_lane(item, j) < item;
+        u32x4 *const counts = reinterpret_cast<u32x4 *>(s.sums);  // a byte a wave for each token
+        uint32_t rank = 0;
+#pragma unroll
+        for (int i = 0; i < SAE_WAVE / NW; ++i) {
+            const int j = wave * (SAE_WAVE / NW) + i;
+            rank += j < n && s.list[j] < item;
+        }
+        reinterpret_cast<uint8_t *>(counts + lane)[wave] = (uint8_t)rank;
+        __syncthreads();
+        if (wave != 0) return;
+        const u32x4 c = counts[lane];
+        rank = 0;
+#pragma unroll
+        for (int i = 0; i < NW / 4; ++i) rank = __builtin_amdgcn_sad_u8(c[i], 0, rank);
         if (lane < n) s.list[rank] = item;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         item = s.list[lane];

@@ -249,7 +249,7 @@ __device__ __forceinline__ Part find_part_tree(const KvDev &c, const AttnArgs &a
     };
     // (in floating point: a quotient of 64-bit numbers is some hundred instructions; at least the quotient)
     auto parts_of = [&](u64 total, int steps) {
-        const int share = max((int)((double)total / plan.groups) + 1, MIN_SPLIT / keys);
+        const int share = max((int)fmin((double)total / plan.groups, 0x1p30) + 1, MIN_SPLIT / keys);  // (more than any tile's steps)
         return min(max((int)((uint32_t)(steps + share / 2) / (uint32_t)share), 1), plan.most);
     };
     if (c.n_seq == 1) {  // uniform
