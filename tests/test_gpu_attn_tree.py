@@ -54,18 +54,22 @@ def test_split_and_not(ty, dim):
 
 
 @pytest.mark.parametrize("ty", TYPES)
-def test_holes(ty):
+@pytest.mark.parametrize("dim", [64, 128])
+def test_holes(ty, dim):
     """Table entries without a block: in the prefix and among the tree's places."""
     lens, new = [100, 64, 40, 33, 500], [20, 64, 1, 33, 50]
     holes = [(0, 0), (0, 3), (1, 3), (3, 0), (3, 1), (3, 2)] + [(4, j) for j in range(4, 24)] + [(4, 30), (2, 1), (0, 5)]
-    TreeCall(ty, 8, 2, 128, lens, new, seed=25, holes=holes).check()
-    TreeCall(ty, 8, 2, 128, lens, new, seed=26, holes=holes, window=30, n_inst=2).check()
+    TreeCall(ty, 8, 2, dim, lens, new, seed=25, holes=holes).check()
+    TreeCall(ty, 8, 2, dim, lens, new, seed=26, holes=holes, window=30, n_inst=2).check()
+    far = [(0, j) for j in range(3, 700, 5)] + [(0, j) for j in range(400, 480)]
+    TreeCall(ty, 4, 1, dim, [11200], [40], seed=27, holes=far).check()
 
 
 @pytest.mark.parametrize("window", [0, 7])
-def test_more_nodes_than_places(window):
+@pytest.mark.parametrize("dim", [64, 128])
+def test_more_nodes_than_places(window, dim):
     """Lengths smaller than the tree (0: padding): nodes without a place see nothing and are not seen."""
-    TreeCall(O.BF16, 8, 2, 128, [5, 20, 0, 300], [40, 25, 3, 30], seed=27, window=window).check()
+    TreeCall(O.BF16, 8, 2, dim, [5, 20, 0, 300], [40, 25, 3, 30], seed=27, window=window).check()
 
 
 def test_one_token_each():
@@ -111,14 +115,15 @@ def test_scale_of_zero_and_below(scale):
 @pytest.mark.parametrize("what", [np.nan, np.inf])
 @pytest.mark.parametrize("window", [0, 40])
 @pytest.mark.parametrize("ty", TYPES)
-def test_values_that_are_not_finite_reach_only_their_descendants(ty, window, what):
+@pytest.mark.parametrize("dim", [64, 128])
+def test_values_that_are_not_finite_reach_only_their_descendants(ty, window, what, dim):
     """NaN or infinity among the values of some nodes and of a prefix key that a window hides from deep rows."""
-    dim, lens, new = 128, np.array([150, 90, 4000]), np.array([60, 90, 30])
+    lens, new = np.array([150, 90, 4000]), np.array([60, 90, 30])
     c = TreeCall(ty, 4, 2, dim, lens, new, kinds=["random", "chain", "binary"], seed=40, window=window)
     size = 1 if ty == O.FP8 else 2
     bits = {(O.BF16, True): 0x7FC0, (O.BF16, False): 0x7F80, (O.F16, True): 0x7E00, (O.F16, False): 0x7C00}
     page = O.unpack(c.cache.pages[1], dim, size, 1)
-    at = [(0, 140, 5), (0, 120, 64), (1, 80, 127), (1, 60, 0), (2, 3990, 3)]
+    at = [(0, 140, 5), (0, 120, dim // 2), (1, 80, dim - 1), (1, 60, 0), (2, 3990, 3)]
     if window:
         at += [(0, 89 - 38, 9)]
     for r, t, d in at:
@@ -173,11 +178,11 @@ def test_bad_parents_are_reported():
         assert api.status_names(int(c.cache.status[0])) == ["BAD_TREE"]
 
 
-@pytest.mark.parametrize("ty", [O.BF16, O.FP8])
-def test_graph_replays_with_new_trees(ty):
+@pytest.mark.parametrize("ty,dim", [(O.BF16, 128), (O.FP8, 128), (O.F16, 64)])
+def test_graph_replays_with_new_trees(ty, dim):
     """A captured call replayed with other lengths, trees and contents equals the eager one, bit for bit."""
     most, new = np.array([3000, 40, 17, 5000, 640]), np.array([30, 1, 2, 64, 5])
-    c = TreeCall(ty, 8, 2, 128, most, new, seed=56)
+    c = TreeCall(ty, 8, 2, dim, most, new, seed=56)
     kv, lens = c.cache.device(), dev32(most - 10)
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
@@ -205,3 +210,14 @@ def test_graph_replays_with_new_trees(ty):
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
     assert int(c.cache.status[0]) == 0
+
+
+@pytest.mark.parametrize("ty,dim", [(O.BF16, 128), (O.F16, 64)])
+def test_more_sequences_than_are_split(ty, dim):
+    """Every sequence in one part, though some are long."""
+    rng = np.random.default_rng(3)
+    new = rng.integers(0, 4, 600)
+    cached = rng.integers(0, 40, 600)
+    cached[[0, 300, 599]] = 2500
+    new[[0, 300, 599]] = 33
+    TreeCall(ty, 4, 2, dim, new + cached, new, seed=60).check()
