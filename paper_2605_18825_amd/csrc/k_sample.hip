@@ -89,7 +89,7 @@ struct Shared {
     double power[PER_TWO];  // 2^(-j / 32) units
     u64 part[2][16];
     float edges[8];
-    uint32_t n, found, want;
+    uint32_t n, found;
 };
 
 // f over the workgroup, in every thread; which: alternates between calls.
@@ -945,36 +945,34 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 4) k_sample(Args
     bool whole = false;  // `total` is the weight of all tokens, and top-k leaves them all
     u64 total = 0;
     if (!SPLIT && k > 0 && k <= SMALL_K<THREADS>) {
-        // the k-th largest of the threads' maxima, to 16 bits of its key
+        // the k-th largest of the threads' maxima, to 16 bits of its key; every wave finds it by itself
         uint32_t bound = 0, want = (uint32_t)k;
         const uint32_t key = key_of(mine);
+        for (int i = threadIdx.x; i < 512; i += THREADS) s.digits.count[i] = 0;
+        if (threadIdx.x == 0) s.n = 0;
+        __syncthreads();
 #pragma unroll 1
         for (int shift = 24; shift >= 16; shift -= 8) {
-            for (int i = threadIdx.x; i < 256; i += THREADS) s.digits.count[i] = 0;
-            if (threadIdx.x == 0) s.n = 0;
+            uint32_t *const count = s.digits.count + (shift == 16 ? 256 : 0);
+            if (shift == 24 || key >> 24 == bound >> 24) atomicAdd(&count[key >> shift & 255], 1u);
             __syncthreads();
-            if (shift == 24 || key >> 24 == bound >> 24) atomicAdd(&s.digits.count[key >> shift & 255], 1u);
-            __syncthreads();
-            if (wave == 0) {
-                uint32_t c[4], sum = 0;
+            uint32_t c[4], sum = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    c[i] = s.digits.count[lane * 4 + i];
-                    sum += c[i];
-                }
-                uint32_t before = sum_upto(sum) - sum;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (before < want && before + c[i] >= want) {
-                        s.found = lane * 4 + i;
-                        s.want = want - before;
-                    }
-                    before += c[i];
-                }
+            for (int i = 0; i < 4; ++i) {
+                c[i] = count[lane * 4 + i];
+                sum += c[i];
             }
-            __syncthreads();
-            bound |= s.found << shift;
-            want = s.want;
+            uint32_t before = sum_upto(sum) - sum;
+            const int at = __builtin_ctzll(__ballot(before < want && before + sum >= want));
+            uint32_t digit = lane * 4;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const bool past = digit == (uint32_t)(lane * 4 + i) && before + c[i] < want;
+                before += past ? c[i] : 0;
+                digit += past;
+            }
+            bound |= of_lane(digit, at) << shift;
+            want -= of_lane(before, at);
         }
         const float least = fmaxf(logit_of(bound | 0xFFFFu), -0x1.fffffep127f);  // (-inf is not taken)
         row.some(least, [&](float l, int i) {
