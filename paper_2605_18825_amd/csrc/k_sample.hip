@@ -826,7 +826,7 @@ __device__ __forceinline__ void fill_powers(Shared &s)
 
 // The first launch of few rows: maxima of the row's groups, 256 a workgroup, and an empty histogram.
 template <int DT>
-__global__ void __launch_bounds__(256) k_sample_max(Args a)
+__global__ void __launch_bounds__(256) k_draw_max(Args a)
 {
     __shared__ float part[4];
     const int r = blockIdx.y;
@@ -852,7 +852,7 @@ __global__ void __launch_bounds__(256) k_sample_max(Args a)
 
 // The second: a part of the row's vectors into the histogram.
 template <int DT>
-__global__ void __launch_bounds__(512) k_sample_hist(Args a, int maxes)
+__global__ void __launch_bounds__(512) k_draw_hist(Args a, int maxes)
 {
     __shared__ Shared s;
     const int r = blockIdx.y;
@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(512) k_sample_hist(Args a, int maxes)
 
 // (Four waves a SIMD, two workgroups of 512 a compute unit: 700 rows of 50,001 at 130 registers 90 us, at 120 72.5.)
 template <int DT, int THREADS, bool SPLIT>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 4) k_sample(Args a)
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 4) k_draw(Args a)
 {
     constexpr int NW = THREADS / SAE_WAVE;
     __shared__ Shared s;
@@ -1135,14 +1135,14 @@ void launch(const Args &a, int rows, hipStream_t s)
 {
     if (is_split(rows, a.vocab) && !a.top_k) {
         const int vectors = a.vocab / Row<DT, 256>::E, maxes = std::min((vectors + 255) / 256, SPLIT_MAXES);
-        hipLaunchKernelGGL((k_sample_max<DT>), dim3(maxes, rows), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_draw_max<DT>), dim3(maxes, rows), dim3(256), 0, s, a);
         // about two workgroups per compute unit, of at least 4 vectors a thread
         const int parts = std::max(std::min(512 / rows, vectors / 2048), 1);
-        hipLaunchKernelGGL((k_sample_hist<DT>), dim3(parts, rows), dim3(512), 0, s, a, maxes);
-        hipLaunchKernelGGL((k_sample<DT, 1024, true>), dim3(rows), dim3(1024), 0, s, a);
-    } else if (a.vocab <= 8192) hipLaunchKernelGGL((k_sample<DT, 256, false>), dim3(rows), dim3(256), 0, s, a);
-    else if (rows >= 512) hipLaunchKernelGGL((k_sample<DT, 512, false>), dim3(rows), dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((k_sample<DT, 1024, false>), dim3(rows), dim3(1024), 0, s, a);
+        hipLaunchKernelGGL((k_draw_hist<DT>), dim3(parts, rows), dim3(512), 0, s, a, maxes);
+        hipLaunchKernelGGL((k_draw<DT, 1024, true>), dim3(rows), dim3(1024), 0, s, a);
+    } else if (a.vocab <= 8192) hipLaunchKernelGGL((k_draw<DT, 256, false>), dim3(rows), dim3(256), 0, s, a);
+    else if (rows >= 512) hipLaunchKernelGGL((k_draw<DT, 512, false>), dim3(rows), dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_draw<DT, 1024, false>), dim3(rows), dim3(1024), 0, s, a);
 }
 
 }  // namespace

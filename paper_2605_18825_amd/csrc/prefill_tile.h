@@ -246,6 +246,7 @@ __device__ __forceinline__ Part find_part_tree(const KvDev &c, const AttnArgs &a
         const int len = kv::seq_len(c, r);
         tiles = (int)((uint32_t)(tokens * G + rows - 1) / (uint32_t)rows);
         steps = (a.window > 0 ? min(a.window + tokens, len) : len) / keys + 1;
+        if (tokens > a.max_nodes) steps = 0;  // its rows see nothing; the join looks at no more than max_nodes' rows
     };
     // (in floating point: a quotient of 64-bit numbers is some hundred instructions; at least the quotient)
     auto parts_of = [&](u64 total, int steps) {

@@ -221,3 +221,27 @@ def test_more_sequences_than_are_split(ty, dim):
     cached[[0, 300, 599]] = 2500
     new[[0, 300, 599]] = 33
     TreeCall(ty, 4, 2, dim, new + cached, new, seed=60).check()
+
+
+@pytest.mark.parametrize("ty,dim", [(O.BF16, 128), (O.F16, 64), (O.FP8, 256)])
+def test_too_many_nodes_behind_a_long_prefix(ty, dim):
+    """All rows of a sequence with more than max_nodes are zeros, where keys are split too; the others are as ever."""
+    lens, new = np.array([3000, 2000, 5000]), np.array([200, 1, 1])
+    for seqs in (slice(0, 1), slice(0, 3)):
+        c = TreeCall(ty, 2, 2, dim, lens[seqs], new[seqs], seed=61)
+        c.max_nodes = 1
+        kv = c.cache.device()
+        q = torch.as_tensor(c.qbits).view(DT[c.dtype]).cuda()
+        out, lse = torch.full_like(q, 7.0), torch.full((c.n, 2), 7.0, device="cuda")
+        work = torch.full((api.sae_attn_work_size(kv, api.make_seqs(dev32(c.ids), dev32(c.lens), q_start=dev32(c.starts)), c.n, 2),), 0xFF,
+                          dtype=torch.uint8, device="cuda")
+        say("too many nodes: type %d dim %d, %d sequences" % (ty, dim, len(c.lens)))
+        api.sae_attn_tree(kv, api.make_seqs(dev32(c.ids), dev32(c.lens), q_start=dev32(c.starts)), c.parent(), 1, q, out, c.scale, work,
+                          lse=lse)
+        want, wl, mag, big = c.want()
+        want[:200], mag[:200], wl[:200] = 0, 0, -np.inf
+        tol, _ = O.bounds(want, wl, mag, big, dim, c.dtype)
+        tol[:200] = 0
+        assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol)
+        assert np.array_equal(np.isinf(lse.cpu().numpy()), np.isinf(wl))
+        assert api.status_names(int(c.cache.status[0])) == ["BAD_TREE"]
