@@ -813,7 +813,7 @@ struct Settings {
     __device__ __forceinline__ bool greedy() const { return !(T > 0.0f) || k == 1 || p <= 0.0f; }
 };
 template <int THREADS>
-constexpr int SMALL_K = THREADS / 4;  // a k that the threads' maxima bound
+constexpr int SMALL_K = THREADS / 2;  // a k that the threads' maxima bound (256 rows of 131,072, k 300: 25.9 us, by the histogram 76.4)
 
 __device__ __forceinline__ Scale scale_of_row(float top, float T, const double *power)
 {
@@ -1140,8 +1140,16 @@ void launch(const Args &a, int rows, hipStream_t s)
         const int parts = std::max(std::min(512 / rows, vectors / 2048), 1);
         hipLaunchKernelGGL((k_draw_hist<DT>), dim3(parts, rows), dim3(512), 0, s, a, maxes);
         hipLaunchKernelGGL((k_draw<DT, 1024, true>), dim3(rows), dim3(1024), 0, s, a);
-    } else if (a.vocab <= 8192) hipLaunchKernelGGL((k_draw<DT, 256, false>), dim3(rows), dim3(256), 0, s, a);
-    else if (rows >= 512) hipLaunchKernelGGL((k_draw<DT, 512, false>), dim3(rows), dim3(512), 0, s, a);
+        return;
+    }
+    // Threads of a row (bf16 logits, top-p, us with 256 / 512 / 1,024: 600 rows of 4,000 17.3 / 22.7 / 37.4, of 8,192 21.5 /
+    // 26.2 / 44.9; 64 rows of 4,000 13.6 / 13.8 / 17.9; 300 rows of 16,000 26.1 / 24.5 / 34.7, of 50,000 57.9 / 52.3 /
+    // 59.5; 64 rows of 16,000 22.9 / 18.8 / 23.3, of 32,000 34.2 / 26.0 / 28.1; one row of 16,000 16.4 / 13.3 / 14.7, of
+    // 50,000 35.7 / 25.7 / 24.5; with 512 / 1,024: 256 rows of 131,072 82.7 / 76.4, 400 rows 115.9 / 130.9, with settings by
+    // row 159 / 135).
+    const bool half = rows >= 512 || a.vocab <= 16384 || (rows > 16 && a.vocab < 65536);
+    if (a.vocab <= 8192) hipLaunchKernelGGL((k_draw<DT, 256, false>), dim3(rows), dim3(256), 0, s, a);
+    else if (half) hipLaunchKernelGGL((k_draw<DT, 512, false>), dim3(rows), dim3(512), 0, s, a);
     else hipLaunchKernelGGL((k_draw<DT, 1024, false>), dim3(rows), dim3(1024), 0, s, a);
 }
 
