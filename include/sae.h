@@ -724,7 +724,7 @@ sae_status sae_attn_tree(const sae_kv *kv, const sae_seqs *seqs, int32_t n_token
  * and always the first.  A temperature that is not above 0 keeps the first alone.  The row's
  * token is the first, in that order, up to which the kept weights' sum passes u times
  * the sum of all of them.  Logits that are NaN or -inf are not taken; where +inf is the
- * largest, tokens that have it share the weight evenly.
+ * largest, tokens that have it share the weight evenly at any temperature above 0.
  *  token[n_rows]     device int32 out; -1 for a row without a token
  *  prob[n_rows]      device float out or NULL: the token's share of the kept weights (0 without one)
  *  kept[n_rows]      device int32 out or NULL: the number of kept tokens

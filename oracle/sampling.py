@@ -12,7 +12,7 @@ def weights(logits, ids, T):
     l = np.asarray(logits, np.float64)[ids]
     with np.errstate(over="ignore", invalid="ignore"):
         w = np.exp((l - l[0]) / float(T))
-    return np.where(l == l[0], 1.0, w)  # also where l[0] is infinite
+    return np.where(l == l[0], 1.0, 0.0 if np.isinf(l[0]) else w)  # the infinite ones share the weight at any T
 
 
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):

@@ -815,9 +815,10 @@ struct Settings {
 template <int THREADS>
 constexpr int SMALL_K = THREADS / 2;  // a k that the threads' maxima bound (256 rows of 131,072, k 300: 25.9 us, by the histogram 76.4)
 
-__device__ __forceinline__ Scale scale_of_row(float top, float T, const double *power)
+// infinite: of a row whose logits are mapped(); T = 1 takes all weight from the ones below the largest (a T past 5e36 leaves them some).
+__device__ __forceinline__ Scale scale_of_row(float top, float T, bool infinite, const double *power)
 {
-    return {(double)top, PER_TWO * 1.44269504088896340736 / (double)T, power};
+    return {(double)top, PER_TWO * 1.44269504088896340736 / (infinite ? 1.0 : (double)T), power};
 }
 __device__ __forceinline__ void fill_powers(Shared &s)
 {
@@ -873,7 +874,7 @@ __global__ void __launch_bounds__(512) k_draw_hist(Args a, int maxes)
         row.infinite = true;
         row.edge = row.mapped(row.edge);
     }
-    const Scale sc = scale_of_row(row.infinite ? 0.0f : top, set.T, s.power);
+    const Scale sc = scale_of_row(row.infinite ? 0.0f : top, set.T, row.infinite, s.power);
     uint32_t light = 0;
     auto put = [&](float l, int) {
         double rest;
@@ -938,7 +939,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 4) k_draw(Args a
         if (threadIdx.x == 0) answer(first, 1.0f, 1);
         return;
     }
-    const Scale sc = scale_of_row(top, set.T, s.power);
+    const Scale sc = scale_of_row(top, set.T, row.infinite, s.power);
 
     // the list: the first tokens of the order, enough of them for every question
     int n = LIST + 1;    // in the list; more than LIST: not collected
