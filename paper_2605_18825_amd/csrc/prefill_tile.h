@@ -278,8 +278,9 @@ __device__ __forceinline__ Part find_part_tree(const KvDev &c, const AttnArgs &a
     u64 total = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) total += sums[0][w];
-    // three sums in one: workgroups (24 bits), split tiles (20), their parts (20)
-    auto packed = [](u64 tiles, u64 parts) { return tiles * parts << 40 | (parts > 1 ? tiles << 20 | tiles * parts : 0); };
+    // three sums in one: workgroups (44 bits), split tiles (10), their parts (10).  No q_start passes them: rows counted again for
+    // several sequences are 512 times 2^23 tiles at most, and 2/3 and 4/3 of 512 groups bound the others whatever is summed.
+    auto packed = [](u64 tiles, u64 parts) { return tiles * parts << 20 | (parts > 1 ? tiles << 10 | tiles * parts : 0); };
     u64 count = 0;
 #pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
@@ -297,22 +298,25 @@ __device__ __forceinline__ Part find_part_tree(const KvDev &c, const AttnArgs &a
     }
 #pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
-        const int rest = x - (int)(before >> 40);
+        const long long rest = x - (long long)(before >> 20);
         if (rest >= 0 && rest < tiles[i] * steps[i]) {  // one thread
             found_seq = r0 + i;
-            found_rest = rest;
+            found_rest = (int)rest;
             found_parts = steps[i];
             found = before;
         }
         before += packed(tiles[i], steps[i]);
     }
     __syncthreads();
-    const int clear = x >= (int)(all >> 20 & 0xFFFFF) ? x : -1;
-    if (x >= (int)(all >> 40)) return {-1, 0, 1, 0, -1, -1, clear};
+    // A q_start that decreases may call for more workgroups than the grid has, a split tile's first one among them: no tile is
+    // noted then, or the join would go by an entry that nobody wrote.
+    const bool over = all >> 20 > (u64)(plan.groups + plan.tiles);
+    const int clear = over || x >= (int)(all >> 10 & 0x3FF) ? x : -1;
+    if (x >= (long long)(all >> 20)) return {-1, 0, 1, 0, -1, -1, clear};
     const int parts = uniform(found_parts), rest = uniform(found_rest), sub = (int)((uint32_t)rest / (uint32_t)parts);
     const u64 at = (u64)uniform((long long)found);
-    return {uniform(found_seq), rest - sub * parts, parts, sub, parts > 1 ? (int)(at & 0xFFFFF) + rest : -1,
-            parts > 1 && rest == sub * parts ? (int)(at >> 20 & 0xFFFFF) + sub : -1, clear};
+    return {uniform(found_seq), rest - sub * parts, parts, sub, parts > 1 ? (int)(at & 0x3FF) + rest : -1,
+            !over && parts > 1 && rest == sub * parts ? (int)(at >> 10 & 0x3FF) + sub : -1, clear};
 }
 
 // A split tile as the workspace has it, by the workgroup of its first part.
