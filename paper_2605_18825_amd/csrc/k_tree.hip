@@ -26,11 +26,14 @@ constexpr int stage_keys(int dim) { return 8192 / (dim * 2); }  // 8 KB of keys,
 
 // 16 bytes per lane from memory to LDS, lane l's to `to` + 16 l, with nothing that the compiler would wait for by
 // itself: it takes every read of LDS for one of what such a load brings, and would wait for the stages ahead (53.3 us
-// for the ragged batch above).  Nothing else in the kernel uses m0.
+// for the ragged batch above).  m0 (the address, read as the load issues) is left as it was: the compiler takes it for reserved and
+// does not heed it among the clobbers, and may keep an address of its own there for such loads as to_lds().
 __device__ __forceinline__ void ring_load(const char *from, char *to)
 {
     const uint32_t at = (uint32_t)uniform((int)(uintptr_t)(__attribute__((address_space(3))) char *)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(at), "v"(from) : "memory");
+    uint32_t held;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(held) : "s"(at), "v"(from) : "memory");
 }
 
 // A barrier at which all but the wave's `LATER` newest loads have arrived, and what it read from LDS or wrote there.
