@@ -811,14 +811,15 @@ struct Settings {
     {
     }
     __device__ __forceinline__ bool greedy() const { return !(T > 0.0f) || k == 1 || p <= 0.0f; }
+    // Of mapped() logits: at T = 1 the ones below the largest weigh nothing (a T past 5e36 would leave them something).
+    __device__ __forceinline__ void set_infinite() { T = T > 0.0f ? 1.0f : T; }
 };
 template <int THREADS>
 constexpr int SMALL_K = THREADS / 2;  // a k that the threads' maxima bound (256 rows of 131,072, k 300: 25.9 us, by the histogram 76.4)
 
-// infinite: of a row whose logits are mapped(); T = 1 takes all weight from the ones below the largest (a T past 5e36 leaves them some).
-__device__ __forceinline__ Scale scale_of_row(float top, float T, bool infinite, const double *power)
+__device__ __forceinline__ Scale scale_of_row(float top, float T, const double *power)
 {
-    return {(double)top, PER_TWO * 1.44269504088896340736 / (infinite ? 1.0 : (double)T), power};
+    return {(double)top, PER_TWO * 1.44269504088896340736 / (double)T, power};
 }
 __device__ __forceinline__ void fill_powers(Shared &s)
 {
@@ -857,7 +858,7 @@ __global__ void __launch_bounds__(512) k_draw_hist(Args a, int maxes)
 {
     __shared__ Shared s;
     const int r = blockIdx.y;
-    const Settings set(a, r);
+    Settings set(a, r);
     if (set.greedy()) return;  // uniform: not asked for
     Row<DT, 512> row(static_cast<const char *>(a.logits) + (int64_t)r * a.stride * Row<DT, 512>::SIZE, a.vocab);
     Shelf &shelf = reinterpret_cast<Shelf *>(a.work)[r];
@@ -873,8 +874,9 @@ __global__ void __launch_bounds__(512) k_draw_hist(Args a, int maxes)
     if (top == __builtin_inff()) {
         row.infinite = true;
         row.edge = row.mapped(row.edge);
+        set.set_infinite();
     }
-    const Scale sc = scale_of_row(row.infinite ? 0.0f : top, set.T, row.infinite, s.power);
+    const Scale sc = scale_of_row(row.infinite ? 0.0f : top, set.T, s.power);
     uint32_t light = 0;
     auto put = [&](float l, int) {
         double rest;
@@ -907,7 +909,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 4) k_draw(Args a
     __shared__ Shared s;
     const int r = blockIdx.x, lane = (int)__lane_id(), wave = threadIdx.x / SAE_WAVE;
     Row<DT, THREADS> row(static_cast<const char *>(a.logits) + (int64_t)r * a.stride * Row<DT, THREADS>::SIZE, a.vocab);
-    const Settings set(a, r);
+    Settings set(a, r);
     const float p = set.p, m = set.m, u = set.u;
     const int k = SPLIT ? 0 : set.k;  // (rows with a top_k are not split)
     auto answer = [&](uint32_t token, float prob, uint32_t kept) {
@@ -929,6 +931,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 4) k_draw(Args a
         row.set_infinite();
         mine = row.mapped(mine);
         top = 0.0f;
+        set.set_infinite();
     }
     if (set.greedy()) {  // the first of the largest
         uint32_t first = ~0u;
@@ -939,7 +942,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 4) k_draw(Args a
         if (threadIdx.x == 0) answer(first, 1.0f, 1);
         return;
     }
-    const Scale sc = scale_of_row(top, set.T, row.infinite, s.power);
+    const Scale sc = scale_of_row(top, set.T, s.power);
 
     // the list: the first tokens of the order, enough of them for every question
     int n = LIST + 1;    // in the list; more than LIST: not collected
