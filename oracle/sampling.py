@@ -4,8 +4,9 @@ import numpy as np
 
 def order(logits):
     """Indexes of the tokens that may be taken, by falling logit, the lower index first."""
-    ids = [i for i in range(len(logits)) if logits[i] > -np.inf]  # false for NaN
-    return sorted(ids, key=lambda i: (-logits[i], i))
+    l = np.asarray(logits, np.float64)
+    ids = np.flatnonzero(l > -np.inf)  # false for NaN
+    return ids[np.argsort(-l[ids], kind="stable")].tolist()
 
 
 def weights(logits, ids, T):
