@@ -673,10 +673,12 @@ sae_status sae_attn_prefill(const sae_kv *kv, const sae_seqs *seqs, int32_t n_to
  *         place in the sequence (the tokens of a tree); or NULL: the place
  *  k, v   as in sae_kv_write; values are stored as they are
  *  q, q_out  device, [n_tokens][n_heads][head_dim] of `dtype`, strides and alignment as for
- *         k: the turned queries; may be the same array; n_heads 1 .. 1024, or n_heads = 0 and
- *         both NULL
+ *         k: the turned queries; n_heads 1 .. 1024, or n_heads = 0 and both NULL.  q_out may be
+ *         q itself, with q's stride; otherwise the rows of q, k and v and those of q_out share no
+ *         value (they may lie side by side in wider rows of one stride, as slices of a fused
+ *         projection do; with different strides the arrays lie apart as a whole)
  * A token without a place (see sae_seqs) is not written and its q_out row is zeros; one
- * whose block is not there is not written.  q_out may not overlap k, v or the cache.
+ * whose block is not there is not written.  q_out may not overlap the cache.
  */
 typedef struct {
     const float *inv_freq;

@@ -596,6 +596,17 @@ static const char *rows_args(const void *p, int64_t stride, int64_t row)
     return nullptr;
 }
 
+// Whether two arrays of n rows of 16-bit values share no value.  (With different strides: whether they lie apart as a whole.)
+static bool rows_apart(const void *p, int64_t p_stride, int64_t p_row, const void *q, int64_t q_stride, int64_t q_row, int64_t n)
+{
+    const uint64_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    const uint64_t a_end = a + 2 * (uint64_t)((n - 1) * p_stride + p_row), b_end = b + 2 * (uint64_t)((n - 1) * q_stride + q_row);
+    if (a_end <= b || b_end <= a) return true;
+    if (n == 1 || p_stride != q_stride) return false;
+    const uint64_t s = 2 * (uint64_t)p_stride, from = a <= b ? (b - a) % s : (s - (a - b) % s) % s;  // of q's rows in p's
+    return from >= 2 * (uint64_t)p_row && from + 2 * (uint64_t)q_row <= s;
+}
+
 static sae_status kv_move_args(const sae_kv *kv, const sae_seqs *sq, int32_t n, int32_t dtype, const void *k,
                                int64_t k_stride, const void *v, int64_t v_stride, KvDev &d)
 {
@@ -652,6 +663,12 @@ sae_status sae_kv_append(const sae_kv *kv, const sae_seqs *seqs, int32_t n_token
         const char *msg = rows_args(q, q_stride, row);
         if (!msg) msg = rows_args(q_out, q_out_stride, row);
         if (msg) return bad(msg);
+        const int64_t kv_row = (int64_t)kv->n_kv_heads * kv->head_dim;
+        const bool in_place = q == q_out && (q_stride == q_out_stride || n_tokens == 1);
+        if ((!in_place && !rows_apart(q, q_stride, row, q_out, q_out_stride, row, n_tokens)) ||
+            !rows_apart(k, k_stride, kv_row, q_out, q_out_stride, row, n_tokens) ||
+            !rows_apart(v, v_stride, kv_row, q_out, q_out_stride, row, n_tokens))
+            return bad("q_out must lie apart from q, k and v, or be q with q's stride");
     }
     if (n_tokens == 0) return SAE_OK;
     const AppendArgs a = {rope, pos, n_heads, q, k, v, q_out, q_stride, q_out_stride, k_stride, v_stride};
