@@ -731,7 +731,8 @@ sae_status sae_attn_tree(const sae_kv *kv, const sae_seqs *seqs, int32_t n_token
  *  prob[n_rows]      device float out or NULL: the token's share of the kept weights (0 without one)
  *  kept[n_rows]      device int32 out or NULL: the number of kept tokens
  *  work              device scratch of at least sae_sample_work_size bytes, 16-byte aligned, as
- *                    for sae_attn_decode
+ *                    for sae_attn_decode; a call's serves every one with no more rows and no
+ *                    larger vocabulary
  * Weights are computed in 64 bits and summed as whole multiples of 2^-43: results do not depend
  * on the order of sums or on how rows are divided over the GPU, and a token or a
  * border is another one than with exact sums only where one lies within vocab * 2^-43 of the other.

@@ -1132,7 +1132,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 4) k_draw(Args a
 // Rows whose passes are launches of their own: from 65,536 tokens and to 64 rows (one row of 131,072 bf16 logits
 // with top-p: 47.0 us as one launch, 26.4 as three; 64 rows 70.9 and 58.1; 64 rows of 64,000 43.7 and 43.4, 200
 // rows of 131,072 81.5 and 94.1), but not with a top_k: rows with a small k read theirs once (14.6 us instead of 10.3).
-bool is_split(int rows, int vocab) { return vocab >= 65536 && rows <= 64; }
+constexpr int SPLIT_VOCAB = 65536, SPLIT_ROWS = 64;
+bool is_split(int rows, int vocab) { return vocab >= SPLIT_VOCAB && rows <= SPLIT_ROWS; }
 
 template <int DT>
 void launch(const Args &a, int rows, hipStream_t s)
@@ -1159,7 +1160,11 @@ void launch(const Args &a, int rows, hipStream_t s)
 
 }  // namespace
 
-size_t sample_work_bytes(int rows, int vocab) { return rows > 0 && is_split(rows, vocab) ? rows * sizeof(Shelf) : 16; }
+// (More rows are not split, but a workspace that was made for them serves fewer ones, which are.)
+size_t sample_work_bytes(int rows, int vocab)
+{
+    return rows > 0 && vocab >= SPLIT_VOCAB ? std::min(rows, SPLIT_ROWS) * sizeof(Shelf) : 16;
+}
 
 hipError_t launch_sample(int rows, int vocab, int dtype, const SampleArgs &x, hipStream_t s)
 {
