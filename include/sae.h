@@ -705,7 +705,9 @@ sae_status sae_kv_append(const sae_kv *kv, const sae_seqs *seqs, int32_t n_token
  * kv_len - n), its ancestors and itself, with window > 0 those whose position is above its own
  * minus the window, and where they have a block and a place.  Sums, roundings, rows that see nothing,
  * values that are not finite, q, out, lse, scale, work and the limit on rows are as in
- * sae_attn_prefill; a chain (parent[j] = j - 1) gives its results.
+ * sae_attn_prefill; a chain (parent[j] = j - 1) gives its results within both's rounding.
+ * Long sequences are split over the GPU and their parts joined in calls of up to 512 sequences and where the
+ * table holds more than 512 keys; a larger batch with a few long sequences is faster as several calls.
  */
 #define SAE_TREE_MAX 256
 sae_status sae_attn_tree(const sae_kv *kv, const sae_seqs *seqs, int32_t n_tokens, const int32_t *parent, int32_t max_nodes,
@@ -723,7 +725,9 @@ sae_status sae_attn_tree(const sae_kv *kv, const sae_seqs *seqs, int32_t n_token
  * lower index first among equal ones; token i weighs w_i = exp((l_i - l_0) / T), l_0 the largest.
  * Kept are: the first k (k <= 0: all); of these the shortest head of the order whose weight
  * is at least p of theirs (p >= 1 or NaN: all); of these the ones with w_i >= m (m <= 0 or NaN: all);
- * and always the first.  A temperature that is not above 0 keeps the first alone.  The row's
+ * and always the first.  A temperature that is not above 0 keeps the first alone.  (An array of
+ * settings that leave everything gives what NULL gives, but without a top_k up to 64 rows of 65,536
+ * and more tokens are divided over several workgroups, with one they are not.)  The row's
  * token is the first, in that order, up to which the kept weights' sum passes u times
  * the sum of all of them.  Logits that are NaN or -inf are not taken; where +inf is the
  * largest, tokens that have it share the weight evenly at any temperature above 0.

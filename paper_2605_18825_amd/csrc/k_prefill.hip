@@ -2,7 +2,8 @@
 // prefill_tile.h.
 #include "prefill_tile.h"
 
-// Enough for every call: keys are split only where there are no more tiles than groups_of(dim) in all.
+// Enough for every call: 2 groups of a head's slots (see plan_of: groups + tiles of a prefill, which has no more tiles than groups
+// where it splits any; 4/3 groups of a tree's call).
 size_t prefill_work_bytes(int kvh, int dim)
 {
     const size_t groups = (size_t)std::max(groups_of(dim) / kvh, 1) * 2;

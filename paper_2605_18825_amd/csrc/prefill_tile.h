@@ -165,7 +165,7 @@ struct Part {
     // a number that no tile has, for this workgroup to say so
     int entry, clear;
 };
-constexpr int PER_THREAD = 2;  // sequences of a thread at most: no more than tiles, which are 512 at most
+constexpr int PER_THREAD = 2;  // sequences of a thread at most: plan_of() splits nothing of a call with more than 512
 
 template <int NW>
 __device__ __forceinline__ Part find_part(const KvDev &c, const AttnArgs &a, const Plan &plan, int x, int rows, int keys)
@@ -324,16 +324,24 @@ struct Split {
     int token, head0, rows;  // token: row of the call's arrays of its first token
     int parts;               // in workgroups x .. x + parts - 1; < 2: none
 };
+// The same for a tree's call, whose split tiles and their parts are numbered by themselves.
+struct TreeSplit {
+    int token;
+    int shape;  // head0 | rows << 16
+    int slot;   // the first part's place in the workspace, the others behind it
+    int parts;  // < 2: none
+};
+static_assert(sizeof(TreeSplit) == sizeof(Split), "they take the same room");
 
 // What a workgroup of a tree's call notes of its part for the join.
 __device__ __forceinline__ void note_split(const AttnArgs &a, const Plan &plan, const Part &p, const Tile &t, int kvhead)
 {
     if (kvhead != 0 || threadIdx.x != 0) return;
-    Split *const at = static_cast<Split *>(a.work);  // {token, head0 | rows << 16, place of the first part, parts}
+    TreeSplit *const at = static_cast<TreeSplit *>(a.work);
     // (no place is written past the last)
-    if (p.clear >= 0 && p.clear < plan.joins) at[p.clear] = Split{0, 0, 0, 0};
+    if (p.clear >= 0 && p.clear < plan.joins) at[p.clear] = TreeSplit{0, 0, 0, 0};
     if (p.entry >= 0 && p.entry < plan.joins)
-        at[p.entry] = Split{t.first + t.token0, t.head0 | t.rows << 16, p.slot, p.slot + p.parts <= plan.slots ? p.parts : 0};
+        at[p.entry] = TreeSplit{t.first + t.token0, t.head0 | t.rows << 16, p.slot, p.slot + p.parts <= plan.slots ? p.parts : 0};
 }
 
 // A step's keys or values on their way from the cache to LDS: 16-byte pieces of
@@ -538,8 +546,9 @@ __device__ void redo(const KvDev &c, const AttnArgs &a, const Tile &t, const Mas
     }
 }
 
-// The workspace: descriptions of workgroups 0 .. groups + tiles - 1, then per
-// workgroup, head and wave a part's outputs, maxima and sums as the lanes hold them.
+// The workspace: plan.slots descriptions, then per slot, head and wave a part's outputs, maxima and sums as the lanes
+// hold them.  Prefill: a slot and a Split for each of workgroups 0 .. groups + tiles - 1.  Trees: a slot for each part of a
+// split tile, and the first plan.joins descriptions are the split tiles' TreeSplits.
 __device__ __forceinline__ float *parts_of(const AttnArgs &a, const Plan &plan)
 {
     return reinterpret_cast<float *>(static_cast<Split *>(a.work) + plan.slots);
@@ -1206,8 +1215,8 @@ __global__ void __launch_bounds__(4 * SAE_WAVE) k_tree_join(KvDev c, AttnArgs a,
     __shared__ float2 mls[NW][SAE_WAVE];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / SAE_WAVE), b = blockIdx.y, tile = blockIdx.z;
     const int kvhead = blockIdx.x % c.kvh, G = a.heads / c.kvh;
-    const Split t = static_cast<const Split *>(a.work)[blockIdx.x / c.kvh];
-    const int head0 = t.head0 & 0xFFFF, rows = t.head0 >> 16, slot = t.rows;
+    const TreeSplit t = static_cast<const TreeSplit *>(a.work)[blockIdx.x / c.kvh];
+    const int head0 = t.shape & 0xFFFF, rows = t.shape >> 16, slot = t.slot;
     if (t.parts < 2 || tile * ROWS >= rows) return;
     const int lane = (int)__lane_id(), n = lane & 31, h = lane >> 5;
     const int row = tile * ROWS + n;
@@ -1266,10 +1275,14 @@ int64_t tiles_of(const KvDev &c, int heads)
     return c.qs ? c.n_tokens * G / rows + c.n_seq : c.n_seq * ((G + rows - 1) / rows);
 }
 
-// Keys are split only where there are no more tiles than groups_of(dim), which bounds the
-// workspace.  With more, a long tile is one workgroup's: 64 sequences of 64 new tokens, 32
-// heads on 8, one behind 32,768 keys and the others behind 1,024, take 632 us, with the
+// A prefill's keys are split only where there are no more tiles than groups_of(dim), which bounds the
+// workspace: groups + tiles slots a head, at most 2 groups.  With more, a long tile is one workgroup's: 64 sequences of 64
+// new tokens, 32 heads on 8, one behind 32,768 keys and the others behind 1,024, take 632 us, with the
 // same keys spread evenly 162.
+// A tree's are split with any number of tiles: slots are numbered among the parts of split tiles, 4/3 groups at most, of 2/3
+// groups tiles (find_part_tree).
+// Neither's where a call has more than 512 sequences (PER_THREAD for each thread to look at) or a table of SHORT keys: 512 trees
+// of 4 nodes behind 196 tokens, four of them behind 15,996, 32 heads on 8, 164 us, 513 of them 404.
 Plan plan_of(const KvDev &c, int heads, int dim, int window, int nodes)
 {
     Plan p = {(int)tiles_of(c, heads), 0, 1, 0, 0};
