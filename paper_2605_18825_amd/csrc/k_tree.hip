@@ -12,8 +12,9 @@
 // sequences of up to 201 nodes behind up to 12,000 tokens, window 4,097, 12 heads: 46.7 us by the other loop, 41.3;
 // with heads of 128 both take the same: 60 us for 32 sequences of 16..32 nodes behind 512..2,048, 90 for 64 of 2).
 //
-// Bound by memory (few rows) or by starts and ends: those 32 sequences, 183 MB, take 52 us, of which 10 are
-// a workgroup's start (its part found, 2 us; table, queries and first keys, 3; the tree, 1) and end, and 5 for the join.  Wide
+// Bound by memory (few rows) or by parts of uneven size, their starts and ends: those 32 sequences, 183 MB, take 52 us, for the
+// longest part of 16 steps (mean 10.9); 10 are a workgroup's start (its part found, 2 us; table, queries and first keys, 3; the tree,
+// 1) and end, and 5 more the join.  The ragged batch above is 780 workgroups, two rounds, of up to 17 steps, mean 8.5.  Wide
 // trees are bound by products: 64 nodes behind 16,385..32,768 tokens of an 8-bit cache, 28 heads on 4, 0.70
 // PFLOP/s.  Built and taken out: all rows in each wave's registers and keys straight from memory to them (k_decode.hip's
 // way): 10 % faster with 8 rows, as fast with 32, 73 us instead of 54 with 64.
