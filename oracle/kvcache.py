@@ -152,9 +152,8 @@ def tree_seen(parent, total, there, window):
         for up, i in enumerate(way):
             if base + i >= 0 and (not window or pos - up > pos - window):
                 seen[j, base + i] = True
-        for t in range(max(base, 0)):
-            if not window or t > pos - window:
-                seen[j, t] = True
+        prefix = np.arange(max(base, 0))
+        seen[j, prefix] = True if not window else prefix > pos - window
     return seen & there[None, :]
 
 
@@ -170,13 +169,15 @@ def tree_attention(q, parent, k, v, there, scale, window):
         at = np.nonzero(seen[i])[0]
         if not len(at):
             continue
-        for u in range(heads):
-            kk, vv = k[at, u // (heads // kvh)], v[at, u // (heads // kvh)]
-            s = scale * (kk @ q[i, u])
-            w = np.exp(s - s.max())
-            out[i, u], mag[i, u] = (w @ vv) / w.sum(), (w @ np.abs(vv)) / w.sum()
-            lse[i, u] = s.max() + np.log(w.sum())
-            big[i, u] = abs(scale) * (np.abs(kk) @ np.abs(q[i, u])).max()
+        for h in range(kvh):
+            kk, vv = k[at, h], v[at, h]
+            ka, va = np.abs(kk), np.abs(vv)
+            for u in range(h * (heads // kvh), (h + 1) * (heads // kvh)):
+                s = scale * (kk @ q[i, u])
+                w = np.exp(s - s.max())
+                out[i, u], mag[i, u] = (w @ vv) / w.sum(), (w @ va) / w.sum()
+                lse[i, u] = s.max() + np.log(w.sum())
+                big[i, u] = abs(scale) * (ka @ np.abs(q[i, u])).max()
     return out, lse, mag, big
 
 
